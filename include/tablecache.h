@@ -333,9 +333,140 @@ tc_status tc_set_attn_kernel(tc_ctx *ctx, int32_t kind);
 int32_t tc_attn_kernel(const tc_ctx *ctx);
 
 /*
+ * Token steps that stay on the GPU.  Everything above takes a batch's lengths and block tables from the host and plans
+ * them there; the calls below take them from DEVICE memory, allocate nothing, wait for nothing and keep no state, so a step -
+ * or a loop of them - can be captured into a graph once and replayed while the sequences grow:
+ *
+ *   tc_step_tables     lengths -> block tables, and request, position and slot of each new token
+ *   tc_rope_append     queries and keys encoded by position, keys and values put into their slots     (every layer)
+ *   tc_digest_blocks   8-bit bounds of the keys of blocks that became full                            (every layer)
+ *   tc_select_blocks   the blocks each token reads, by a cheap score of those bounds                  (every layer, or some)
+ *   tc_block_attn      attention of the token over the listed blocks                                  (every layer)
+ *
+ * Sequences are those of tc_stitch_kv, tc_stitch_kv_rope and tc_stitch_alias: tc_table_entries turns their block tables into
+ * device entries (copied to the GPU by the caller), tc_grow_seqs on a table row of its own hands out the spare blocks,
+ * tc_release_seqs takes all of them back.  The pool's blocks are as tc_prefill_attn leaves them, so both kinds of call can
+ * take turns on a sequence.
+ *
+ * Conventions of these calls.  Integer arrays are int32 (slots int64) in DEVICE memory unless said otherwise; a call
+ * cannot look at them, so what they hold is checked on the GPU: a row that names no request, position or block is passed
+ * over, and nothing outside the arrays and the pool is read or written.  Every call must be made with the context's
+ * device current (else TC_ERR_INVALID) and on a stream ordered behind whatever produced its inputs; calls on different streams
+ * may overlap if their outputs and workspaces are different.  Tables that sequences read in place (tc_stitch_alias) must stay
+ * pinned until the last such call has been enqueued, for replays of a captured graph until those are done.
+ * Limits: 8192 requests and 2^20 tokens in a call, max_blocks <= 2^26, fewer than 2^27 pool blocks.
+ *
+ * Block layout.  In layer l, K of block b is [Hkv][16][D]; V behind it is [Hkv][16][D] in fp32 and [Hkv][D][16] in bf16, there with
+ * token t at position (t & 3) | (t & 4) << 1 | (t & 8) >> 1.  Sequence blocks of a layer stand behind one another.
+ *
+ * Device block tables.  [B][max_blocks]: block id, with the number of its unused tail positions in bits 27 and up (blocks of
+ * table slots, tc_stitch_alias), -1: none.
+ */
+
+/* HOST block_table [n] (ids, -1 = none) -> HOST entries [n].  Errors: TC_ERR_INVALID if an id is beyond the pool, or below
+ * tc_first_seq_block and no block of a loaded table (nothing is written). */
+tc_status tc_table_entries(tc_ctx *ctx, const int32_t *block_table, int64_t n, int32_t *entries);
+
+/*
+ * One step's tables from the requests' lengths: request b holds seq_len[b] tokens and brings new_len[b] (0: it waits).  Its row
+ * gets blocks for positions [seq_len[b], seq_len[b] + new_len[b]) behind the ceil(seq_len[b] / 16) it has: the entries
+ * spare[spare_used[0]], spare[spare_used[0] + 1], .. in order, requests in order.  Tokens are numbered request by
+ * request, in position order.
+ *   spare [n_spare]         ids of sequence blocks to take; one that is none becomes -1 in the row, its tokens get no slot
+ *   spare_used, spare_next  [1] entries taken before, and behind, this step (may be the same address)
+ *   end_len [B]             seq_len + new_len (may be seq_len itself, which then advances)
+ *   cu_new [B + 1]          first token of each request, and the number of tokens
+ *   slot_map, token_pos, token_seq, full_block [n_tokens]
+ *                           16 * block + position % 16; position; request; the block's id where the token takes its last slot,
+ *                           else -1.  Rows behind the step's tokens are -1 in all four.
+ *   status [2]              0 (or an error of this list), and the number of blocks taken:
+ *                           TC_ERR_OOM_POOL   the spare entries do not suffice (status[1]: how many blocks the step takes)
+ *                           TC_ERR_INVALID    a length is negative or ends beyond max_blocks * 16, more than n_tokens new
+ *                                             tokens, or spare_used is no place of spare
+ *                           Then the tables, the lengths and spare_next stay as seq_len and spare_used have them, and the step has
+ *                           no tokens: every call that is given its rows does nothing.
+ * The arrays must not overlap except as said.
+ */
+tc_status tc_step_tables(tc_ctx *ctx, const int32_t *seq_len, const int32_t *new_len, int32_t B, int32_t *block_table,
+                         int32_t max_blocks, const int32_t *spare, int32_t n_spare, const int32_t *spare_used,
+                         int32_t *spare_next, int32_t *end_len, int32_t *cu_new, int64_t *slot_map, int32_t *token_pos,
+                         int32_t *token_seq, int32_t *full_block, int32_t n_tokens, int32_t *status, void *stream);
+
+/*
+ * Encode a layer's queries and keys by position, and append keys and values.  In every head of q and k, elements (j, j + D/2) are
+ * turned by pos_a(n) * rope_theta^(-2j/D) radians, as tc_stitch_kv_rope does with stored keys; a is the axis of pair j: the
+ * first sections[0] pairs belong to axis 0, the next sections[1] to axis 1, and so on (time, height, width of
+ * multi-axis positions; with one axis all pairs).  The turn is reduced in fp64, the rotation is fp32, the result is rounded once.
+ * Keys and values go to slot slot_map[n] of the pool.
+ *   q [n_tokens][Hq][D], k, v [n_tokens][Hkv][D]   DEVICE, element strides q_stride, k_stride, v_stride from row to row (parts of
+ *               one projection's rows, say); rows start at multiples of 16 bytes
+ *   pos         [n_axes][n_tokens], any int32;  n_axes 1 .. 4;  sections HOST [n_axes], D/2 in sum (NULL: one axis)
+ *   slot_map    [n_tokens]; a row whose slot is negative, or in no sequence block, is passed over (q_out too)
+ *   q_out       [n_tokens][Hq][D] (may be q, where q_stride is Hq * D)
+ * Tokens of one block must stand in position order, as tc_step_tables lists them, and no slot twice.  A block whose first slot
+ * is written gets zeros behind the last of these tokens, so that no later call finds leftovers there.
+ */
+tc_status tc_rope_append(tc_ctx *ctx, int32_t layer, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                         const void *v, int64_t v_stride, const int32_t *pos, int32_t n_axes, const int32_t *sections,
+                         double rope_theta, const int64_t *slot_map, int32_t n_tokens, void *q_out, void *stream);
+
+/*
+ * Digests: for every layer, KV head and block of the pool, bounds of its keys.  With hi_d and lo_d the largest and smallest value
+ * of channel d among the block's tokens, and e the smallest integer >= -126 for which no |hi_d| or |lo_d| exceeds 127 * 2^e:
+ * int8 ceil(hi_d / 2^e) and floor(lo_d / 2^e), and e; zeros and e = 127 if a key is not finite.
+ *   digests    DEVICE, tc_digest_bytes(cfg) bytes, 16-byte aligned, the caller's: bounds int8 [L][Hkv][n_pool_blocks][2][D]
+ *              (hi, lo), then exponents int8 [L][Hkv][n_pool_blocks]
+ *   entries    [n] entries of device block tables (a whole table, or tc_step_tables' full_block); -1 is passed over.  A block's unused
+ *              tail positions take no part.
+ * Layers [l0, l1).  tc_select_blocks reads the digests of full blocks only.
+ */
+size_t tc_digest_bytes(const tc_config *cfg);
+tc_status tc_digest_blocks(tc_ctx *ctx, int32_t l0, int32_t l1, const int32_t *entries, int32_t n, void *digests, void *stream);
+
+/* Bytes of workspace (256-byte aligned, contents need not be initialised and are not kept) for tc_select_blocks and
+ * tc_block_attn of up to n_tokens tokens.  tc_select_blocks makes do with less, down to n_kv_heads * max_blocks * 4.
+ * 0: an argument out of range. */
+size_t tc_sparse_workspace_bytes(const tc_config *cfg, int32_t n_tokens, int32_t max_blocks, int32_t n_list);
+
+/*
+ * The blocks that a token attends to, for each KV head: the first n_sink of its sequence, the last n_local up to the one
+ * that holds its own position, and between these the n_top blocks with the highest scores.  A block's score is the
+ * largest, over the query heads of the KV head, of
+ *     2^e 2^f sum_d (max(i_d, 0) hi_d + min(i_d, 0) lo_d),    i_d = q_d / 2^f rounded to nearest even,
+ * f chosen for the head's query as e is for a block's keys: up to the rounding of q, no key of the block scores higher.
+ * It is the product in fp32 of an integer below 2^24 with two powers of two, so it does not depend on the order of sums; equal
+ * scores go to the lower block.  A block with a key that is not finite scores +infinity; a head whose query is not
+ * finite takes no part (if none does, and for entries that name no block: -infinity).
+ *   q             [n_tokens][Hq][D], as tc_rope_append leaves them
+ *   token_seq, token_pos   [n_tokens]; rows whose request or position is none are passed over
+ *   lists         [n_tokens][Hkv][n_sink + n_top + n_local], out: logical blocks in ascending order, then -1
+ * The blocks before the token's last n_local must have digests.
+ * Errors: TC_ERR_INVALID; TC_ERR_CAPACITY (workspace).
+ */
+tc_status tc_select_blocks(tc_ctx *ctx, int32_t layer, const void *q, const int32_t *token_seq, const int32_t *token_pos,
+                           int32_t n_tokens, const int32_t *block_table, int32_t B, int32_t max_blocks, const void *digests,
+                           int32_t n_sink, int32_t n_top, int32_t n_local, int32_t *lists, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
+/*
+ * Attention over listed blocks: for token n at position p of its sequence, head h (KV head h / (Hq/Hkv)),
+ *     out = softmax_j( sm_scale * q . k_j ) v_j   over the keys at positions j <= p of the blocks in its list;
+ * rows with no such key, or whose weights are all zero, are zeros.  Positions that the token does not see - behind its own, and
+ * the unused tail of a table block - have no influence, whatever values stand there.
+ *   lists         [n_tokens][Hkv][n_list]: logical blocks of the token's sequence in any order - from tc_select_blocks (of this
+ *                 layer or an earlier one) or of the caller's own making.  -1, blocks behind the token's own and entries that
+ *                 name no block are passed over; a block listed twice is attended to twice.
+ *   out           [n_tokens][Hq][D]; rows whose request or position is none are left as they are
+ * Errors: TC_ERR_INVALID; TC_ERR_CAPACITY (workspace; none is needed where tc_sparse_workspace_bytes' partials are zero).
+ */
+tc_status tc_block_attn(tc_ctx *ctx, int32_t layer, const void *q, const int32_t *token_seq, const int32_t *token_pos,
+                        int32_t n_tokens, const int32_t *block_table, int32_t B, int32_t max_blocks, const int32_t *lists,
+                        int32_t n_list, void *out, float sm_scale, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Measurement support.  With profiling on, every kernel the library launches carries two HIP
  * events that receive the begin and end timestamps of its own dispatch on the stream it is launched
- * on (no extra packets between kernels).  tc_profile_read waits for them and returns, per kernel kind (0 stitch, 1 append where it is a launch of its own (no kernel's is), 2 attention, 3 split-KV merge), the summed
+ * on (no extra packets between kernels).  tc_profile_read waits for them and returns, per kernel kind (0 stitch, 1 append where it is a launch of its own (tc_rope_append), 2 attention, 3 split-KV merge), the summed
  * elapsed milliseconds and the number of launches since the previous read.
  *   ms_out HOST double[4], count_out HOST int64_t[4].
  */

@@ -45,7 +45,9 @@ EXPORTS = ["tc_block_bytes", "tc_pool_bytes", "tc_first_seq_block", "tc_create",
            "tc_stitch_kv", "tc_stitch_kv_rope", "tc_stitch_alias", "tc_prefill_attn", "tc_prefill_attn_noalloc", "tc_grow_seqs", "tc_release_seqs", "tc_read_seq_kv",
            "tc_kv_splits", "tc_set_kv_splits", "tc_set_row_blocks", "tc_set_attn_kernel", "tc_attn_kernel", "tc_profile_enable", "tc_profile_read", "tc_last_error", "tc_version",
            "tc_trie_create", "tc_trie_destroy", "tc_trie_insert", "tc_trie_match", "tc_rerank",
-           "tc_pin_tables", "tc_unpin_tables", "tc_plan_pipeline"]
+           "tc_pin_tables", "tc_unpin_tables", "tc_plan_pipeline",
+           "tc_table_entries", "tc_step_tables", "tc_rope_append", "tc_digest_bytes", "tc_digest_blocks",
+           "tc_sparse_workspace_bytes", "tc_select_blocks", "tc_block_attn"]
 
 
 class tc_config(ctypes.Structure):
@@ -96,6 +98,14 @@ _sig = {
     "tc_pin_tables": (_i32, [_vp, _vp, _i32]),
     "tc_unpin_tables": (_i32, [_vp, _vp, _i32]),
     "tc_plan_pipeline": (_i32, [_vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _i32]),
+    "tc_table_entries": (_i32, [_vp, _vp, _i64, _vp]),
+    "tc_step_tables": (_i32, [_vp, _vp, _vp, _i32, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp]),
+    "tc_rope_append": (_i32, [_vp, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i32, _vp, ctypes.c_double, _vp, _i32, _vp, _vp]),
+    "tc_digest_bytes": (ctypes.c_size_t, [_cfgp]),
+    "tc_digest_blocks": (_i32, [_vp, _i32, _i32, _vp, _i32, _vp, _vp]),
+    "tc_sparse_workspace_bytes": (ctypes.c_size_t, [_cfgp, _i32, _i32, _i32]),
+    "tc_select_blocks": (_i32, [_vp, _i32, _vp, _vp, _vp, _i32, _vp, _i32, _i32, _vp, _i32, _i32, _i32, _vp, _vp, ctypes.c_size_t, _vp]),
+    "tc_block_attn": (_i32, [_vp, _i32, _vp, _vp, _vp, _i32, _vp, _i32, _i32, _vp, _i32, _vp, ctypes.c_float, _vp, ctypes.c_size_t, _vp]),
 }
 for _n, (_r, _a) in _sig.items():
     getattr(_lib, _n).restype = _r
@@ -136,6 +146,18 @@ def _stream(s) -> Optional[int]:
     return s.cuda_stream       # torch.cuda.Stream
 
 
+def _dev(t, dtype, *shape) -> int:
+    """Address of a contiguous device tensor of that type and shape (device arrays are read by what their neighbours say
+    of their length, so one that is too short must not get through)."""
+    if t.dtype is not dtype or tuple(t.shape) != shape or not t.is_contiguous() or not t.is_cuda:
+        raise TcError(TC_ERR_INVALID, "expected a contiguous device tensor %s %s, got %s %s" % (
+            dtype, list(shape), t.dtype, list(t.shape)))
+    return t.data_ptr()
+
+
+_TORCH_TYPE = {TC_F32: torch.float32, TC_BF16: torch.bfloat16}
+
+
 def make_config(n_layers, n_q_heads, n_kv_heads, head_dim, dtype, n_pool_blocks, table_capacity,
                 max_table_tokens, policy=TC_POLICY_LRU, block_size=16, slot_layout=TC_SLOTS_ROWS) -> tc_config:
     return tc_config(n_layers, n_q_heads, n_kv_heads, head_dim, block_size, dtype, n_pool_blocks,
@@ -152,6 +174,14 @@ def tc_pool_bytes(cfg: tc_config) -> int:
 
 def tc_first_seq_block(cfg: tc_config) -> int:
     return int(_lib.tc_first_seq_block(ctypes.byref(cfg)))
+
+
+def tc_digest_bytes(cfg: tc_config) -> int:
+    return int(_lib.tc_digest_bytes(ctypes.byref(cfg)))
+
+
+def tc_sparse_workspace_bytes(cfg: tc_config, n_tokens: int, max_blocks: int, n_list: int) -> int:
+    return int(_lib.tc_sparse_workspace_bytes(ctypes.byref(cfg), n_tokens, max_blocks, n_list))
 
 
 def tc_version() -> str:
@@ -173,6 +203,7 @@ class Context:
         self._h = h
         self._addr = h.value
         self._keep = []                           # registered host KV
+        self._digest_bytes = tc_digest_bytes(cfg)
 
     def _check(self, rc: int):
         if rc != TC_OK:
@@ -282,6 +313,73 @@ class Context:
         self._check(_lib.tc_read_seq_kv(self._h, layer, blk.ctypes.data, n_tokens, k.ctypes.data,
                                         v.ctypes.data, _stream(stream)))
         return k, v
+
+    # ---- token steps on the device: every array a torch tensor on the context's GPU, sizes taken from their shapes
+    def tc_table_entries(self, block_table) -> np.ndarray:
+        """Device block-table entries of a host block table (to be copied to the GPU)."""
+        bt = _i32arr(block_table)
+        out = np.empty_like(bt)
+        self._check(_lib.tc_table_entries(self._h, bt.ctypes.data, bt.size, out.ctypes.data))
+        return out
+
+    def tc_step_tables(self, seq_len, new_len, block_table, spare, spare_used, spare_next, end_len, cu_new, slot_map,
+                       token_pos, token_seq, full_block, status, stream=None):
+        i32 = torch.int32
+        n_seq, max_blocks = block_table.shape
+        n, n_spare = slot_map.shape[0], spare.shape[0]
+        self._check(_lib.tc_step_tables(
+            self._h, _dev(seq_len, i32, n_seq), _dev(new_len, i32, n_seq), n_seq, _dev(block_table, i32, n_seq, max_blocks), max_blocks,
+            _dev(spare, i32, n_spare), n_spare, _dev(spare_used, i32, 1), _dev(spare_next, i32, 1), _dev(end_len, i32, n_seq),
+            _dev(cu_new, i32, n_seq + 1), _dev(slot_map, torch.int64, n), _dev(token_pos, i32, n), _dev(token_seq, i32, n),
+            _dev(full_block, i32, n), n, _dev(status, i32, 2), _stream(stream)))
+
+    def _rows(self, t, n, heads):
+        """(address, elements from row to row) of a tensor [n][heads][D] whose rows may stand apart."""
+        d = self.cfg.head_dim
+        if t.dtype is not _TORCH_TYPE[self.cfg.dtype] or tuple(t.shape) != (n, heads, d) or not t.is_cuda or \
+                (t.numel() and t.stride()[1:] != (d, 1)):
+            raise TcError(TC_ERR_INVALID, "expected device rows [%d][%d][%d] of the context's type, got %s %s" % (
+                n, heads, d, t.dtype, list(t.shape)))
+        return t.data_ptr(), t.stride(0) if n > 1 else heads * d
+
+    def tc_rope_append(self, layer: int, q, k, v, pos, rope_theta: float, slot_map, q_out, sections=None, stream=None):
+        """pos: int32 [n_tokens], or [axes][n_tokens] with the pairs of each axis in `sections`."""
+        c, n = self.cfg, slot_map.shape[0]
+        axes = 1 if pos.dim() == 1 else pos.shape[0]
+        sec = None if sections is None else _i32arr(sections)
+        if sec is not None and sec.size != axes:
+            raise TcError(TC_ERR_INVALID, "%d sections for %d axes" % (sec.size, axes))
+        (qp, qs), (kp, ks), (vp, vs) = self._rows(q, n, c.n_q_heads), self._rows(k, n, c.n_kv_heads), self._rows(v, n, c.n_kv_heads)
+        self._check(_lib.tc_rope_append(
+            self._h, layer, qp, qs, kp, ks, vp, vs, _dev(pos, torch.int32, *((n,) if pos.dim() == 1 else (axes, n))), axes,
+            None if sec is None else sec.ctypes.data, rope_theta, _dev(slot_map, torch.int64, n), n,
+            _dev(q_out, q.dtype, n, c.n_q_heads, c.head_dim), _stream(stream)))
+
+    def tc_digest_blocks(self, l0: int, l1: int, entries, digests, stream=None):
+        """entries: any int32 tensor of block-table entries; digests: tc_digest_bytes(cfg) bytes."""
+        self._check(_lib.tc_digest_blocks(self._h, l0, l1, _dev(entries, torch.int32, *entries.shape), entries.numel(),
+                                          _dev(digests, torch.int8, self._digest_bytes), _stream(stream)))
+
+    def tc_select_blocks(self, layer: int, q, token_seq, token_pos, block_table, digests, n_sink: int, n_top: int, n_local: int,
+                         lists, workspace, stream=None):
+        c, i32, n = self.cfg, torch.int32, token_seq.shape[0]
+        n_seq, max_blocks = block_table.shape
+        self._check(_lib.tc_select_blocks(
+            self._h, layer, _dev(q, _TORCH_TYPE[c.dtype], n, c.n_q_heads, c.head_dim), _dev(token_seq, i32, n), _dev(token_pos, i32, n), n,
+            _dev(block_table, i32, n_seq, max_blocks), n_seq, max_blocks, _dev(digests, torch.int8, self._digest_bytes), n_sink, n_top,
+            n_local, _dev(lists, i32, n, c.n_kv_heads, n_sink + n_top + n_local), _dev(workspace, torch.uint8, workspace.numel()),
+            workspace.numel(), _stream(stream)))
+
+    def tc_block_attn(self, layer: int, q, token_seq, token_pos, block_table, lists, out, sm_scale: float, workspace, stream=None):
+        c, i32, n = self.cfg, torch.int32, token_seq.shape[0]
+        n_seq, max_blocks = block_table.shape
+        n_list = lists.shape[2]
+        dt = _TORCH_TYPE[c.dtype]
+        self._check(_lib.tc_block_attn(
+            self._h, layer, _dev(q, dt, n, c.n_q_heads, c.head_dim), _dev(token_seq, i32, n), _dev(token_pos, i32, n), n,
+            _dev(block_table, i32, n_seq, max_blocks), n_seq, max_blocks, _dev(lists, i32, n, c.n_kv_heads, n_list), n_list,
+            _dev(out, dt, n, c.n_q_heads, c.head_dim), sm_scale, _dev(workspace, torch.uint8, workspace.numel()), workspace.numel(),
+            _stream(stream)))
 
     def tc_kv_splits(self) -> int:
         return int(_lib.tc_kv_splits(self._h))

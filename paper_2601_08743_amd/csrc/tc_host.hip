@@ -4,6 +4,7 @@
 #include "../../include/tablecache.h"
 #include "host_logic.h"
 #include "kv_append.h"
+#include "step_ops.h"
 #include "tc_internal.h"
 
 #include <algorithm>
@@ -1078,6 +1079,242 @@ tc_status tc_read_seq_kv(tc_ctx *ctx, int32_t layer, const int32_t *blocks, int3
     if (e == hipSuccess) e = hipStreamSynchronize(stream);
     if (e != hipSuccess) st = fail(ctx, TC_ERR_HIP, "read: %s", hipGetErrorString(e));
     return st;
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------ token steps on the device
+// Scores of a selection are worked off in rounds of tokens; more workspace than this for them is not asked for.
+static constexpr size_t kScoreRoundBytes = size_t(256) << 20;
+
+static int64_t first_pool_block(const tc_config &c)    // the lowest block id whose keys the pool keeps in blocks
+{
+    return c.slot_layout == TC_SLOTS_BLOCKS ? 0 : tc_first_seq_block(&c);
+}
+
+static size_t score_bytes_per_token(const tc_config &c, int32_t max_blocks)
+{
+    return (size_t)c.n_kv_heads * (size_t)max_blocks * sizeof(uint32_t);
+}
+
+static size_t block_part_bytes(const tc_config &c, int32_t n_tokens, int32_t n_list)
+{
+    const int splits = block_attn_splits(c.n_q_heads, c.n_kv_heads, esize_of(c), n_tokens, n_list);
+    return splits <= 1 ? 0 : (size_t)n_tokens * c.n_q_heads * splits * (size_t)(c.head_dim + 2) * sizeof(float);
+}
+
+// What the device-side calls share: limits, the context's own device, and a pool with block ids that leave room for the counts
+// of unused positions.
+static tc_status step_check(tc_ctx *ctx, const char *what, int32_t n_tokens, int32_t B, int32_t max_blocks)
+{
+    if (n_tokens < 0 || n_tokens > kStepMaxTokens) return fail(ctx, TC_ERR_INVALID, "%s: %d tokens (0 .. %d)", what, n_tokens, kStepMaxTokens);
+    if (B < 0 || B > kStepMaxSeqs) return fail(ctx, TC_ERR_INVALID, "%s: %d requests (0 .. %d)", what, B, kStepMaxSeqs);
+    if (max_blocks < 0 || max_blocks > (1 << 26)) return fail(ctx, TC_ERR_INVALID, "%s: max_blocks out of range", what);
+    if (ctx->cfg.n_pool_blocks > (int64_t)kBidMask) return fail(ctx, TC_ERR_INVALID, "%s: block ids of this pool do not fit device block tables", what);
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess) return fail(ctx, TC_ERR_HIP, "%s: no current device", what);
+    if (dev != ctx->device) return fail(ctx, TC_ERR_INVALID, "%s: the current device is %d, the context's is %d", what, dev, ctx->device);
+    return TC_OK;
+}
+
+static tc_status layer_check(tc_ctx *ctx, const char *what, int32_t layer)
+{
+    if (layer < 0 || layer >= ctx->cfg.n_layers) return fail(ctx, TC_ERR_INVALID, "%s: layer %d out of range", what, layer);
+    if (first_pool_block(ctx->cfg) >= ctx->cfg.n_pool_blocks) return fail(ctx, TC_ERR_INVALID, "%s: the pool has no blocks to attend to", what);
+    return TC_OK;
+}
+
+// Launches that may read table slots in place (which, only the device knows): a load that evicts a table waits for them.
+static void slots_read(tc_ctx *ctx, hipStream_t stream)
+{
+    if (ctx->cfg.slot_layout != TC_SLOTS_BLOCKS) return;
+    for (Slot &s : ctx->slots)
+        if (s.table >= 0) { s.reader_stream = stream; s.reader_pending = true; }
+}
+
+static bool misaligned(const void *p, size_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
+
+extern "C" {
+
+size_t tc_digest_bytes(const tc_config *c)
+{
+    if (!config_ok(c)) return 0;
+    return (size_t)c->n_layers * c->n_kv_heads * (size_t)c->n_pool_blocks * (size_t)(2 * c->head_dim + 1);
+}
+
+size_t tc_sparse_workspace_bytes(const tc_config *c, int32_t n_tokens, int32_t max_blocks, int32_t n_list)
+{
+    if (!config_ok(c) || n_tokens < 0 || n_tokens > kStepMaxTokens || max_blocks < 0 || max_blocks > (1 << 26) || n_list < 1) return 0;
+    const size_t one = score_bytes_per_token(*c, max_blocks), all = one * (size_t)n_tokens;
+    const size_t scores = std::min(all, std::max(one, kScoreRoundBytes));
+    return (std::max({scores, block_part_bytes(*c, n_tokens, n_list), size_t(1)}) + 255) & ~size_t(255);
+}
+
+tc_status tc_table_entries(tc_ctx *ctx, const int32_t *block_table, int64_t n, int32_t *entries)
+{
+    if (!ctx) return TC_ERR_INVALID;
+    if (n < 0 || (n > 0 && (!block_table || !entries))) return fail(ctx, TC_ERR_INVALID, "entries: bad arguments");
+    if (ctx->cfg.n_pool_blocks > (int64_t)kBidMask) return fail(ctx, TC_ERR_INVALID, "entries: block ids of this pool do not fit device block tables");
+    for (int pass = 0; pass < 2; ++pass)                 // nothing is written unless every entry is one
+        for (int64_t k = 0; k < n; ++k) {
+            const int32_t b = block_table[k];
+            int32_t pad = 0;
+            if (b >= 0 && b < ctx->first_seq) {
+                pad = ctx->cfg.slot_layout == TC_SLOTS_BLOCKS ? slot_block_pad(ctx, b) : -1;
+                if (pad < 0) return fail(ctx, TC_ERR_INVALID, "entries: block %d (entry %lld) is no block of a loaded table", b, (long long)k);
+            }
+            if (b >= ctx->cfg.n_pool_blocks) return fail(ctx, TC_ERR_INVALID, "entries: block %d (entry %lld) is beyond the pool", b, (long long)k);
+            if (pass == 1) entries[k] = b < 0 ? -1 : (int32_t)((uint32_t)b | ((uint32_t)pad << kPadShift));
+        }
+    return TC_OK;
+}
+
+tc_status tc_step_tables(tc_ctx *ctx, const int32_t *seq_len, const int32_t *new_len, int32_t B, int32_t *block_table,
+                         int32_t max_blocks, const int32_t *spare, int32_t n_spare, const int32_t *spare_used,
+                         int32_t *spare_next, int32_t *end_len, int32_t *cu_new, int64_t *slot_map, int32_t *token_pos,
+                         int32_t *token_seq, int32_t *full_block, int32_t n_tokens, int32_t *status, void *stream)
+{
+    if (!ctx) return TC_ERR_INVALID;
+    const tc_status st = step_check(ctx, "tables", n_tokens, B, max_blocks);
+    if (st != TC_OK) return st;
+    if (n_spare < 0) return fail(ctx, TC_ERR_INVALID, "tables: negative size");
+    if (!spare_used || !spare_next || !cu_new || !status || (n_spare > 0 && !spare) || (B > 0 && (!seq_len || !new_len || !end_len)) ||
+        ((int64_t)B * max_blocks > 0 && !block_table) || (n_tokens > 0 && (!slot_map || !token_pos || !token_seq || !full_block)))
+        return fail(ctx, TC_ERR_INVALID, "tables: null argument");
+    if (misaligned(slot_map, 8)) return fail(ctx, TC_ERR_INVALID, "tables: slot_map must be 8-byte aligned");
+    const StepTables s{seq_len, new_len, block_table, spare, spare_used, spare_next, end_len, cu_new, slot_map, token_pos, token_seq,
+                       full_block, status, B, max_blocks, n_spare, n_tokens, (int32_t)ctx->first_seq, (int32_t)ctx->cfg.n_pool_blocks};
+    TC_HIP(ctx, launch_step_tables(s, Launch{(hipStream_t)stream, nullptr, nullptr}));
+    return TC_OK;
+}
+
+tc_status tc_rope_append(tc_ctx *ctx, int32_t layer, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                         const void *v, int64_t v_stride, const int32_t *pos, int32_t n_axes, const int32_t *sections,
+                         double rope_theta, const int64_t *slot_map, int32_t n_tokens, void *q_out, void *stream)
+{
+    if (!ctx) return TC_ERR_INVALID;
+    tc_status st = step_check(ctx, "append", n_tokens, 0, 0);
+    if (st == TC_OK) st = layer_check(ctx, "append", layer);
+    if (st != TC_OK) return st;
+    const Geom &g = ctx->geom;
+    if (n_axes < 1 || n_axes > kRopeMaxAxes || (n_axes > 1 && !sections)) return fail(ctx, TC_ERR_INVALID, "append: 1 .. %d axes, with the pairs of each", kRopeMaxAxes);
+    if (!(rope_theta > 1.0) || !std::isfinite(rope_theta)) return fail(ctx, TC_ERR_INVALID, "append: rope_theta must be finite and > 1");
+    RopeAppend a{};
+    int64_t pairs = 0;
+    for (int x = 0; x < kRopeMaxAxes; ++x) {
+        if (x < n_axes) {
+            const int32_t width = n_axes == 1 && !sections ? g.D / 2 : sections[x];
+            if (width < 0) return fail(ctx, TC_ERR_INVALID, "append: negative section");
+            pairs += width;
+        }
+        a.section_end[x] = (int32_t)std::min<int64_t>(pairs, g.D / 2);
+    }
+    if (pairs != g.D / 2) return fail(ctx, TC_ERR_INVALID, "append: the sections hold %lld pairs, a head has %d", (long long)pairs, g.D / 2);
+    if (n_tokens == 0) return TC_OK;
+    if (!q || !k || !v || !pos || !slot_map || !q_out) return fail(ctx, TC_ERR_INVALID, "append: null tensor");
+    if (q_stride < (int64_t)g.Hq * g.D || k_stride < (int64_t)g.Hkv * g.D || v_stride < (int64_t)g.Hkv * g.D)
+        return fail(ctx, TC_ERR_INVALID, "append: rows overlap");
+    if (misaligned(q, 16) || misaligned(k, 16) || misaligned(v, 16) || misaligned(q_out, 16) || misaligned(slot_map, 8) ||
+        ((q_stride | k_stride | v_stride) * g.esize & 15))
+        return fail(ctx, TC_ERR_INVALID, "append: rows must be 16-byte aligned");
+    a.q = (const char *)q; a.k = (const char *)k; a.v = (const char *)v;
+    a.q_stride = q_stride * g.esize; a.k_stride = k_stride * g.esize; a.v_stride = v_stride * g.esize;
+    a.q_out = (char *)q_out;
+    a.pos = pos; a.slot_map = slot_map; a.n_tokens = n_tokens; a.layer = layer;
+    RopeFreq f{};
+    const double two_pi = 6.283185307179586476925286766559;
+    for (int j = 0; j < g.D / 2; ++j) f.rev[j] = std::pow(rope_theta, -2.0 * j / g.D) / two_pi;
+    TC_HIP(ctx, timed_launch(ctx, 1, (hipStream_t)stream, [&](const Launch &ln) { return launch_rope_append(g, f, a, ln); }));
+    return TC_OK;
+}
+
+tc_status tc_digest_blocks(tc_ctx *ctx, int32_t l0, int32_t l1, const int32_t *entries, int32_t n, void *digests, void *stream_)
+{
+    if (!ctx) return TC_ERR_INVALID;
+    const tc_status st = step_check(ctx, "digest", 0, 0, 0);
+    if (st != TC_OK) return st;
+    if (l0 < 0 || l1 > ctx->cfg.n_layers || l0 > l1) return fail(ctx, TC_ERR_INVALID, "digest: bad layer range [%d,%d)", l0, l1);
+    if (n < 0) return fail(ctx, TC_ERR_INVALID, "digest: negative size");
+    if (n == 0 || l0 == l1) return TC_OK;
+    if (!entries || !digests) return fail(ctx, TC_ERR_INVALID, "digest: null argument");
+    if (misaligned(digests, 16)) return fail(ctx, TC_ERR_INVALID, "digest: digests must be 16-byte aligned");
+    hipStream_t stream = (hipStream_t)stream_;
+    DigestArgs a{};
+    a.entries = entries; a.digests = (int8_t *)digests; a.n = n; a.l0 = l0;
+    a.exps_at = (int64_t)ctx->cfg.n_layers * ctx->cfg.n_kv_heads * ctx->cfg.n_pool_blocks * 2 * ctx->cfg.head_dim;
+    a.first_block = (int32_t)first_pool_block(ctx->cfg);
+    TC_HIP(ctx, launch_digest(ctx->geom, a, l1, Launch{stream, nullptr, nullptr}));
+    slots_read(ctx, stream);
+    return TC_OK;
+}
+
+tc_status tc_select_blocks(tc_ctx *ctx, int32_t layer, const void *q, const int32_t *token_seq, const int32_t *token_pos,
+                           int32_t n_tokens, const int32_t *block_table, int32_t B, int32_t max_blocks, const void *digests,
+                           int32_t n_sink, int32_t n_top, int32_t n_local, int32_t *lists, void *workspace,
+                           size_t workspace_bytes, void *stream)
+{
+    if (!ctx) return TC_ERR_INVALID;
+    tc_status st = step_check(ctx, "select", n_tokens, B, max_blocks);
+    if (st == TC_OK) st = layer_check(ctx, "select", layer);
+    if (st != TC_OK) return st;
+    if (n_sink < 0 || n_top < 0 || n_local < 1 || (int64_t)n_sink + n_top + n_local > (1 << 26))
+        return fail(ctx, TC_ERR_INVALID, "select: lists of %d + %d + %d blocks (the last at least 1)", n_sink, n_top, n_local);
+    if (n_tokens == 0) return TC_OK;
+    if (!q || !token_seq || !token_pos || !digests || !lists || ((int64_t)B * max_blocks > 0 && !block_table))
+        return fail(ctx, TC_ERR_INVALID, "select: null argument");
+    if (misaligned(q, 16) || misaligned(digests, 16) || misaligned(workspace, 16)) return fail(ctx, TC_ERR_INVALID, "select: tensors must be 16-byte aligned");
+    SelectArgs a{};
+    a.q = (const char *)q; a.token_seq = token_seq; a.token_pos = token_pos; a.block_table = block_table;
+    a.digests = (const int8_t *)digests; a.lists = lists;
+    a.exps_at = (int64_t)ctx->cfg.n_layers * ctx->cfg.n_kv_heads * ctx->cfg.n_pool_blocks * 2 * ctx->cfg.head_dim;
+    a.scores = (uint32_t *)workspace; a.score_stride = max_blocks;
+    a.layer = layer; a.B = B; a.max_blocks = max_blocks; a.n_sink = n_sink; a.n_top = n_top; a.n_local = n_local;
+    a.first_block = (int32_t)first_pool_block(ctx->cfg);
+    int64_t round = n_tokens;
+    if (max_blocks > n_top && n_top > 0) {               // else every candidate is listed, or none
+        const size_t one = score_bytes_per_token(ctx->cfg, max_blocks);
+        if (!workspace || workspace_bytes < one)
+            return fail(ctx, TC_ERR_CAPACITY, "select: the workspace holds %zu bytes, a token's scores take %zu", workspace ? workspace_bytes : 0, one);
+        round = std::min<int64_t>(round, (int64_t)(workspace_bytes / one));
+    }
+    for (int64_t n0 = 0; n0 < n_tokens; n0 += round) {
+        a.n0 = (int32_t)n0;
+        a.n_tokens = (int32_t)std::min<int64_t>(round, n_tokens - n0);
+        TC_HIP(ctx, launch_select(ctx->geom, a, Launch{(hipStream_t)stream, nullptr, nullptr}));
+    }
+    return TC_OK;
+}
+
+tc_status tc_block_attn(tc_ctx *ctx, int32_t layer, const void *q, const int32_t *token_seq, const int32_t *token_pos,
+                        int32_t n_tokens, const int32_t *block_table, int32_t B, int32_t max_blocks, const int32_t *lists,
+                        int32_t n_list, void *out, float sm_scale, void *workspace, size_t workspace_bytes, void *stream_)
+{
+    if (!ctx) return TC_ERR_INVALID;
+    tc_status st = step_check(ctx, "block attn", n_tokens, B, max_blocks);
+    if (st == TC_OK) st = layer_check(ctx, "block attn", layer);
+    if (st != TC_OK) return st;
+    if (!(sm_scale > 0.f) || !std::isfinite(sm_scale)) return fail(ctx, TC_ERR_INVALID, "block attn: sm_scale must be positive and finite");
+    if (n_list < 1 || n_list > (1 << 26)) return fail(ctx, TC_ERR_INVALID, "block attn: lists of %d blocks", n_list);
+    if (n_tokens == 0) return TC_OK;
+    if (!q || !token_seq || !token_pos || !lists || !out || ((int64_t)B * max_blocks > 0 && !block_table))
+        return fail(ctx, TC_ERR_INVALID, "block attn: null argument");
+    if (misaligned(q, 16) || misaligned(out, 16) || misaligned(workspace, 16)) return fail(ctx, TC_ERR_INVALID, "block attn: tensors must be 16-byte aligned");
+    hipStream_t stream = (hipStream_t)stream_;
+    const size_t need = block_part_bytes(ctx->cfg, n_tokens, n_list);
+    if (need > 0 && (!workspace || workspace_bytes < need))
+        return fail(ctx, TC_ERR_CAPACITY, "block attn: the workspace holds %zu bytes, the partials take %zu", workspace ? workspace_bytes : 0, need);
+    BlockAttnArgs a{};
+    a.q = (const char *)q; a.token_seq = token_seq; a.token_pos = token_pos; a.block_table = block_table; a.lists = lists;
+    a.out = (char *)out; a.scale_log2 = sm_scale * 1.4426950408889634f;
+    a.n_tokens = n_tokens; a.layer = layer; a.B = B; a.max_blocks = max_blocks; a.n_list = n_list;
+    a.n_splits = block_attn_splits(ctx->geom.Hq, ctx->geom.Hkv, ctx->geom.esize, n_tokens, n_list);
+    a.first_block = (int32_t)first_pool_block(ctx->cfg);
+    a.part_o = (float *)workspace;
+    if (need > 0) a.part_ml = a.part_o + (size_t)n_tokens * ctx->geom.Hq * a.n_splits * ctx->geom.D;
+    TC_HIP(ctx, timed_launch(ctx, 2, stream, [&](const Launch &ln) { return launch_block_attn(ctx->geom, a, ln); }));
+    if (a.n_splits > 1) TC_HIP(ctx, timed_launch(ctx, 3, stream, [&](const Launch &ln) { return launch_block_merge(ctx->geom, a, ln); }));
+    slots_read(ctx, stream);
+    return TC_OK;
 }
 
 tc_status tc_profile_enable(tc_ctx *ctx, int32_t on)
