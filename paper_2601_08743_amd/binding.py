@@ -1,5 +1,5 @@
 """ctypes binding over libtablecache.so: argument marshalling only (that of the calls made once per layer
-by a small native module, ``csrc/py_call.cpp``).
+by small native modules, ``csrc/py_call.cpp`` and ``csrc/py_step.cpp``).
 
 Every function here has the name of the C entry point it calls (see
 include/tablecache.h for the semantics).  Device tensors are passed as torch
@@ -29,9 +29,9 @@ if not os.path.exists(LIB_PATH):
 
 _lib = ctypes.CDLL(LIB_PATH)
 try:
-    from . import _py_call
+    from . import _py_call, _py_step
 except ImportError as e:
-    raise ImportError("_py_call.so is not built (%s). Run `python -m paper_2601_08743_amd.build`." % e) from e
+    raise ImportError("_py_call.so or _py_step.so is not built (%s). Run `python -m paper_2601_08743_amd.build`." % e) from e
 
 TC_OK = 0
 TC_ERR_INVALID, TC_ERR_UNKNOWN_TABLE, TC_ERR_OOM_POOL = -1, -2, -3
@@ -112,14 +112,18 @@ for _n, (_r, _a) in _sig.items():
     getattr(_lib, _n).argtypes = _a
 
 
-_PREFILL = ctypes.cast(_lib.tc_prefill_attn, ctypes.c_void_p).value
-_PREFILL_NOALLOC = ctypes.cast(_lib.tc_prefill_attn_noalloc, ctypes.c_void_p).value
+_PREFILL, _PREFILL_NOALLOC, _STEP_TABLES, _ROPE_APPEND, _DIGEST_BLOCKS, _SELECT_BLOCKS, _BLOCK_ATTN = (
+    ctypes.cast(f, ctypes.c_void_p).value for f in (_lib.tc_prefill_attn, _lib.tc_prefill_attn_noalloc, _lib.tc_step_tables,
+                                                    _lib.tc_rope_append, _lib.tc_digest_blocks, _lib.tc_select_blocks, _lib.tc_block_attn))
 
 
 class TcError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__("tc error %d: %s" % (code, msg))
         self.code = code
+
+
+_py_step.set_error(TcError)
 
 
 def _ptr(x) -> Optional[int]:
@@ -144,18 +148,6 @@ def _stream(s) -> Optional[int]:
     if s is None or isinstance(s, int):
         return s
     return s.cuda_stream       # torch.cuda.Stream
-
-
-def _dev(t, dtype, *shape) -> int:
-    """Address of a contiguous device tensor of that type and shape (device arrays are read by what their neighbours say
-    of their length, so one that is too short must not get through)."""
-    if t.dtype is not dtype or tuple(t.shape) != shape or not t.is_contiguous() or not t.is_cuda:
-        raise TcError(TC_ERR_INVALID, "expected a contiguous device tensor %s %s, got %s %s" % (
-            dtype, list(shape), t.dtype, list(t.shape)))
-    return t.data_ptr()
-
-
-_TORCH_TYPE = {TC_F32: torch.float32, TC_BF16: torch.bfloat16}
 
 
 def make_config(n_layers, n_q_heads, n_kv_heads, head_dim, dtype, n_pool_blocks, table_capacity,
@@ -203,7 +195,7 @@ class Context:
         self._h = h
         self._addr = h.value
         self._keep = []                           # registered host KV
-        self._digest_bytes = tc_digest_bytes(cfg)
+        self._step = (self._addr, cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim, int(cfg.dtype == TC_BF16), tc_digest_bytes(cfg))
 
     def _check(self, rc: int):
         if rc != TC_OK:
@@ -213,6 +205,7 @@ class Context:
         if self._h:
             _lib.tc_destroy(self._h)
             self._h = self._addr = None
+            self._step = (None,) + self._step[1:]
 
     def __del__(self):
         try:
@@ -324,62 +317,36 @@ class Context:
 
     def tc_step_tables(self, seq_len, new_len, block_table, spare, spare_used, spare_next, end_len, cu_new, slot_map,
                        token_pos, token_seq, full_block, status, stream=None):
-        i32 = torch.int32
-        n_seq, max_blocks = block_table.shape
-        n, n_spare = slot_map.shape[0], spare.shape[0]
-        self._check(_lib.tc_step_tables(
-            self._h, _dev(seq_len, i32, n_seq), _dev(new_len, i32, n_seq), n_seq, _dev(block_table, i32, n_seq, max_blocks), max_blocks,
-            _dev(spare, i32, n_spare), n_spare, _dev(spare_used, i32, 1), _dev(spare_next, i32, 1), _dev(end_len, i32, n_seq),
-            _dev(cu_new, i32, n_seq + 1), _dev(slot_map, torch.int64, n), _dev(token_pos, i32, n), _dev(token_seq, i32, n),
-            _dev(full_block, i32, n), n, _dev(status, i32, 2), _stream(stream)))
-
-    def _rows(self, t, n, heads):
-        """(address, elements from row to row) of a tensor [n][heads][D] whose rows may stand apart."""
-        d = self.cfg.head_dim
-        if t.dtype is not _TORCH_TYPE[self.cfg.dtype] or tuple(t.shape) != (n, heads, d) or not t.is_cuda or \
-                (t.numel() and t.stride()[1:] != (d, 1)):
-            raise TcError(TC_ERR_INVALID, "expected device rows [%d][%d][%d] of the context's type, got %s %s" % (
-                n, heads, d, t.dtype, list(t.shape)))
-        return t.data_ptr(), t.stride(0) if n > 1 else heads * d
+        rc = _py_step.step_tables(_STEP_TABLES, self._step, seq_len, new_len, block_table, spare, spare_used, spare_next, end_len, cu_new,
+                                  slot_map, token_pos, token_seq, full_block, status, stream)
+        if rc != TC_OK:
+            self._check(rc)
 
     def tc_rope_append(self, layer: int, q, k, v, pos, rope_theta: float, slot_map, q_out, sections=None, stream=None):
         """pos: int32 [n_tokens], or [axes][n_tokens] with the pairs of each axis in `sections`."""
-        c, n = self.cfg, slot_map.shape[0]
-        axes = 1 if pos.dim() == 1 else pos.shape[0]
         sec = None if sections is None else _i32arr(sections)
-        if sec is not None and sec.size != axes:
-            raise TcError(TC_ERR_INVALID, "%d sections for %d axes" % (sec.size, axes))
-        (qp, qs), (kp, ks), (vp, vs) = self._rows(q, n, c.n_q_heads), self._rows(k, n, c.n_kv_heads), self._rows(v, n, c.n_kv_heads)
-        self._check(_lib.tc_rope_append(
-            self._h, layer, qp, qs, kp, ks, vp, vs, _dev(pos, torch.int32, *((n,) if pos.dim() == 1 else (axes, n))), axes,
-            None if sec is None else sec.ctypes.data, rope_theta, _dev(slot_map, torch.int64, n), n,
-            _dev(q_out, q.dtype, n, c.n_q_heads, c.head_dim), _stream(stream)))
+        rc = _py_step.rope_append(_ROPE_APPEND, self._step, layer, q, k, v, pos, None if sec is None else sec.ctypes.data,
+                                  0 if sec is None else sec.size, rope_theta, slot_map, q_out, stream)
+        if rc != TC_OK:
+            self._check(rc)
 
     def tc_digest_blocks(self, l0: int, l1: int, entries, digests, stream=None):
         """entries: any int32 tensor of block-table entries; digests: tc_digest_bytes(cfg) bytes."""
-        self._check(_lib.tc_digest_blocks(self._h, l0, l1, _dev(entries, torch.int32, *entries.shape), entries.numel(),
-                                          _dev(digests, torch.int8, self._digest_bytes), _stream(stream)))
+        rc = _py_step.digest_blocks(_DIGEST_BLOCKS, self._step, l0, l1, entries, digests, stream)
+        if rc != TC_OK:
+            self._check(rc)
 
     def tc_select_blocks(self, layer: int, q, token_seq, token_pos, block_table, digests, n_sink: int, n_top: int, n_local: int,
                          lists, workspace, stream=None):
-        c, i32, n = self.cfg, torch.int32, token_seq.shape[0]
-        n_seq, max_blocks = block_table.shape
-        self._check(_lib.tc_select_blocks(
-            self._h, layer, _dev(q, _TORCH_TYPE[c.dtype], n, c.n_q_heads, c.head_dim), _dev(token_seq, i32, n), _dev(token_pos, i32, n), n,
-            _dev(block_table, i32, n_seq, max_blocks), n_seq, max_blocks, _dev(digests, torch.int8, self._digest_bytes), n_sink, n_top,
-            n_local, _dev(lists, i32, n, c.n_kv_heads, n_sink + n_top + n_local), _dev(workspace, torch.uint8, workspace.numel()),
-            workspace.numel(), _stream(stream)))
+        rc = _py_step.select_blocks(_SELECT_BLOCKS, self._step, layer, q, token_seq, token_pos, block_table, digests, n_sink, n_top,
+                                    n_local, lists, workspace, stream)
+        if rc != TC_OK:
+            self._check(rc)
 
     def tc_block_attn(self, layer: int, q, token_seq, token_pos, block_table, lists, out, sm_scale: float, workspace, stream=None):
-        c, i32, n = self.cfg, torch.int32, token_seq.shape[0]
-        n_seq, max_blocks = block_table.shape
-        n_list = lists.shape[2]
-        dt = _TORCH_TYPE[c.dtype]
-        self._check(_lib.tc_block_attn(
-            self._h, layer, _dev(q, dt, n, c.n_q_heads, c.head_dim), _dev(token_seq, i32, n), _dev(token_pos, i32, n), n,
-            _dev(block_table, i32, n_seq, max_blocks), n_seq, max_blocks, _dev(lists, i32, n, c.n_kv_heads, n_list), n_list,
-            _dev(out, dt, n, c.n_q_heads, c.head_dim), sm_scale, _dev(workspace, torch.uint8, workspace.numel()), workspace.numel(),
-            _stream(stream)))
+        rc = _py_step.block_attn(_BLOCK_ATTN, self._step, layer, q, token_seq, token_pos, block_table, lists, out, sm_scale, workspace, stream)
+        if rc != TC_OK:
+            self._check(rc)
 
     def tc_kv_splits(self) -> int:
         return int(_lib.tc_kv_splits(self._h))
