@@ -8,7 +8,7 @@
 #include <algorithm>
 
 #include "arrive.h"
-#include "kv_append.h"
+#include "lds_dma.h"
 #include "step_ops.h"
 
 namespace tc {
@@ -32,127 +32,271 @@ __device__ __forceinline__ bool token_place(const int32_t *token_seq, const int3
     return seq >= 0 && seq < B && pos >= 0 && (pos >> 4) < max_blocks;
 }
 
+// Over lanes 16 and 32 apart, by exchanging rows of a wave (a shuffle through LDS takes ten times as long).
+__device__ __forceinline__ float max_of_quarters(float x)
+{
+    const unsigned u = __float_as_uint(x);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const unsigned v = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
 // ------------------------------------------------------------------------------------ scores
 // i8 matrix instructions, 16 query rows x 16 blocks x 64: A the query rows as [max(qi, 0) | min(qi, 0)], B the bounds [hi | lo]
 // of 16 blocks, straight from memory (a block's 2D bytes are whole lines).  Bound: reading the bounds, 1/16 of the cache's
-// bytes in bf16.  A work-group takes one token and KV head and a range of its candidates, a wave 16 blocks at a time.
-constexpr int kScoreBlocks = 256;                        // candidates of a work-group
+// bytes in bf16.
+template <int kD>
+struct QueryRows {                                       // 16 rows as a wave holds them
+    static constexpr int kSteps = 2 * kD / 64;           // matrix instructions along the 2D products
+    i32x4 a[kSteps];
+    float scale[4];                                      // of rows 4 q4 + e, whose products stand in this lane: 2^f, -1 for a row that takes no part
+};
 
+// Row r16 of this lane: `qr` its channels, `counts` whether it is one.  Lane (r16, q4) holds channels 16 q4 .. and 64 + 16 q4 ..
+// (kD = 64: the first only).
 template <bool kBf16, int kD>
+__device__ __forceinline__ QueryRows<kD> query_rows(const char *qr, bool counts, int q4)
+{
+    constexpr int kSteps = QueryRows<kD>::kSteps;
+    QueryRows<kD> q;
+    float x[kSteps / 2][16];
+    uint32_t size = 0;
+#pragma unroll
+    for (int s = 0; s < kSteps / 2; ++s)
+#pragma unroll
+        for (int c = 0; c < (kBf16 ? 2 : 4); ++c) {
+            const uint4 v = *(const uint4 *)(qr + (64 * s + 16 * q4) * (kBf16 ? 2 : 4) + c * 16);
+            const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (kBf16) {
+                    x[s][8 * c + 2 * k] = __uint_as_float(u[k] << 16);
+                    x[s][8 * c + 2 * k + 1] = __uint_as_float(u[k] & 0xffff0000u);
+                } else {
+                    x[s][4 * c + k] = __uint_as_float(u[k]);
+                }
+            }
+        }
+#pragma unroll
+    for (int s = 0; s < kSteps / 2; ++s)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) size = max(size, __float_as_uint(x[s][k]) & 0x7fffffffu);
+    size = max(size, (uint32_t)__shfl_xor((int)size, 16));
+    size = max(size, (uint32_t)__shfl_xor((int)size, 32));
+    const bool finite = size < 0x7f800000u;
+    const int f = finite ? step_exponent(__uint_as_float(size)) : 0;
+    const float by = step_pow2(-f), two_f = finite && counts ? step_pow2(f) : -1.f;
+#pragma unroll
+    for (int s = 0; s < kSteps / 2; ++s)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            uint32_t plus = 0, minus = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = finite ? (int)rintf(x[s][4 * k + e] * by) : 0;
+                plus |= (uint32_t)max(i, 0) << (8 * e);
+                minus |= ((uint32_t)min(i, 0) & 0xffu) << (8 * e);
+            }
+            q.a[s][k] = (int)plus;
+            q.a[kSteps / 2 + s][k] = (int)minus;
+        }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) q.scale[e] = __shfl(two_f, 4 * q4 + e);
+    return q;
+}
+
+// Whether an entry names a block, and where that block's digest stands among those of the layer and KV head; one that does not reads
+// another's.
+__device__ __forceinline__ bool is_block(const Geom &g, const SelectArgs &a, int32_t entry)
+{
+    return entry >= 0 && entry_bid(entry) >= a.first_block && entry_bid(entry) < g.n_blocks;
+}
+__device__ __forceinline__ int64_t digest_at(const Geom &g, const SelectArgs &a, int kvh, int32_t entry)
+{
+    return ((int64_t)a.layer * g.Hkv + kvh) * g.n_blocks + (is_block(g, a, entry) ? entry_bid(entry) : a.first_block);
+}
+constexpr int kNoBlock = 128;                            // in the place of an exponent; 127 marks a key that is not finite
+__device__ __forceinline__ int block_exponent(const Geom &g, const SelectArgs &a, int kvh, int32_t entry)
+{
+    const int e = a.digests[a.exps_at + digest_at(g, a, kvh, entry)];
+    return is_block(g, a, entry) ? e : kNoBlock;
+}
+
+// The bounds of 16 blocks in LDS: row r of 2D bytes is block r's, its 16-byte chunk c at position c ^ r (so that the operand reads of
+// neighbouring rows meet different banks).  By direct loads of whole rows: read straight as operands, 64 bytes of each of 16 rows
+// at a time, they take a CU's address path four times as long (see the attention below).
+template <int kD>
+struct BoundsTile {
+    static constexpr int kChunks = 2 * kD / 16, kBytes = 16 * 2 * kD, kLoads = kBytes / 1024;
+    uint32_t lds;                                        // 16-byte aligned address of the tile
+    // entry: of block r16, in every quarter of the wave
+    __device__ __forceinline__ void load(const Geom &g, const SelectArgs &a, int kvh, int32_t entry, int lane) const
+    {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int row = i * (64 / kChunks) + lane / kChunks, c = (lane % kChunks) ^ (row % kChunks);
+            load_to_lds_each(lds + i * 1024, (const char *)a.digests + digest_at(g, a, kvh, __shfl(entry, row)) * (2 * kD) + c * 16);
+        }
+    }
+    // The operands of block r16, quarter q4.
+    __device__ __forceinline__ void operands(i32x4 (&b)[QueryRows<kD>::kSteps], int r16, int q4) const
+    {
+        typedef const __attribute__((address_space(3))) i32x4 *lds_chunk;
+#pragma unroll
+        for (int s = 0; s < QueryRows<kD>::kSteps; ++s)
+            b[s] = *(lds_chunk)(uintptr_t)(lds + r16 * (2 * kD) + (((4 * s + q4) ^ (r16 % kChunks)) << 4));
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // tile read out
+    }
+};
+
+// Products of this lane's four rows with its block, each by its row's power of two.
+template <int kD>
+__device__ __forceinline__ f32x4 row_products(const QueryRows<kD> &q, const i32x4 (&b)[QueryRows<kD>::kSteps])
+{
+    i32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+    for (int s = 0; s < QueryRows<kD>::kSteps; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(q.a[s], b[s], acc, 0, 0, 0);
+    f32x4 p;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[e] = q.scale[e] < 0.f ? -INFINITY : (float)acc[e] * q.scale[e];
+    return p;
+}
+__device__ __forceinline__ float column_max(f32x4 p)     // over the 16 rows, in every quarter
+{
+    return max_of_quarters(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])));
+}
+
+// A block's score as bits that order like it: the largest product m of its rows, by the block's own power of two.
+__device__ __forceinline__ uint32_t score_key(float m, int e)
+{
+    m = e == 127 ? INFINITY : e == kNoBlock ? -INFINITY : m * step_pow2(min(e, 126)) + 0.f;       // (+ 0: the two zeros are equal)
+    const uint32_t u = __float_as_uint(m);
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+
+// Scores to memory, where one launch for scores and list (below) does not do: a work-group takes a KV head, kTiles * 16 query rows
+// and a range of candidates, a wave 16 blocks at a time.
+//   kTiles = 1   one token (its heads 16 at a time): tokens of many requests, long tables.  More work-groups than tokens
+//                share the digests.
+//   kTiles = 4   64 / G neighbouring tokens: suffixes, whose tokens read the same digests.  Tokens of another request follow with
+//                a pass of their own.
+constexpr int kScoreBlocks = 512;                        // candidates of a work-group
+
+template <bool kBf16, int kD, int kTiles>
 __global__ __launch_bounds__(256) void score_kernel(Geom g, SelectArgs a)
 {
-    constexpr int kSteps = 2 * kD / 64;                  // matrix instructions along the 2D products
-    const int item = blockIdx.x / a.score_parts, part = blockIdx.x - item * a.score_parts;
-    const int n = a.n0 + item / g.Hkv, kvh = item % g.Hkv;
-    int seq, pos;
-    if (!token_place(a.token_seq, a.token_pos, n, a.B, a.max_blocks, seq, pos)) return;
-    const Window win(pos, a.n_sink, a.n_local);
-    const int j0 = win.first + part * kScoreBlocks;
-    if (win.candidates() <= a.n_top || j0 >= win.w0) return;
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r16 = lane & 15, q4 = lane >> 4;
-    const int32_t *table = a.block_table + (int64_t)seq * a.max_blocks;
-    const int8_t *bounds = a.digests + ((int64_t)a.layer * g.Hkv + kvh) * g.n_blocks * (2 * kD);
-    const int8_t *exps = a.digests + a.exps_at + ((int64_t)a.layer * g.Hkv + kvh) * g.n_blocks;
-    uint32_t *scores = a.scores + ((int64_t)(n - a.n0) * g.Hkv + kvh) * a.score_stride;
-    float best[kScoreBlocks / 64];
+    typedef BoundsTile<kD> Tile;
+    __shared__ __attribute__((aligned(256))) char s_tile[4][2][Tile::kBytes];
+    __shared__ int32_t s_entry[kScoreBlocks], s_exp[kScoreBlocks];
+    __shared__ float s_prod[4][kTiles > 1 ? kTiles * 16 * 17 : 1];
+    __shared__ int2 s_range[kTiles > 1 ? kTiles * 16 : 1];           // the candidates of each token
+    const int group = blockIdx.x / (a.score_parts * g.Hkv), rest = blockIdx.x - group * (a.score_parts * g.Hkv);
+    const int kvh = rest / a.score_parts, part = rest - kvh * a.score_parts;
+    const int n0 = a.n0 + group * a.group_tokens, n1 = min(n0 + a.group_tokens, a.n0 + a.n_tokens);
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, q4 = lane >> 4;
+    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)s_tile[w][0];
+    auto tile = [&](int k) { return Tile{ring + (uint32_t)(k & 1) * Tile::kBytes}; };
+    auto rows_at = [&](int row) {                        // of the group's rows, from `row` on
+        const int r = row + r16, tok = kTiles > 1 ? r / g.G : 0, head = kTiles > 1 ? r - tok * g.G : r;
+        const bool counts = n0 + tok < n1 && head < g.G;
+        return query_rows<kBf16, kD>(a.q + ((int64_t)min(n0 + tok, n1 - 1) * g.Hq + kvh * g.G + min(head, g.G - 1)) * g.head_bytes, counts, q4);
+    };
+    QueryRows<kD> q[kTiles];
+    if (kTiles > 1) {
 #pragma unroll
-    for (int i = 0; i < kScoreBlocks / 64; ++i) best[i] = -INFINITY;
-    for (int row0 = 0; row0 < g.G; row0 += 16) {
-        // lane (row r16, quarter q4) holds channels 16 q4 .. and 64 + 16 q4 .. (kD = 64: the first only) of its row
-        const int row = min(row0 + r16, g.G - 1);
-        const char *qr = a.q + ((int64_t)n * g.Hq + kvh * g.G + row) * g.head_bytes;
-        float x[kSteps / 2][16];
-        uint32_t size = 0;
+        for (int t = 0; t < kTiles; ++t) q[t] = rows_at(16 * t);
+    }
+    for (int t0 = n0, t1; t0 < n1; t0 = t1) {
+        // tokens t0 .. t1 - 1 of one request, and the candidates that one of them chooses from
+        int seq, pos, j0 = INT32_MAX, j1 = 0;
+        for (t1 = t0; t1 < n1; ++t1) {
+            int s, p;
+            const bool ok = token_place(a.token_seq, a.token_pos, t1, a.B, a.max_blocks, s, p);
+            if (!ok) s = -1;
+            if (t1 == t0) seq = s;
+            else if (s != seq) break;
+            if (!ok) continue;
+            const Window win(p, a.n_sink, a.n_local);
+            if (win.candidates() <= a.n_top) continue;
+            j0 = min(j0, win.first);
+            j1 = max(j1, win.w0);
+            pos = p;
+        }
+        if (j1 <= j0 || j0 + part * kScoreBlocks >= j1) continue;
+        j0 += part * kScoreBlocks;
+        const int count = min(kScoreBlocks, j1 - j0), rounds = count > 16 * w ? (count - 16 * w + 63) >> 6 : 0;
+        const int32_t *table = a.block_table + (int64_t)seq * a.max_blocks + j0;
+        __syncthreads();                                 // (another request's entries were read)
+        if (kTiles > 1 && t0 + tid < t1) {
+            int s, p;
+            const bool ok = token_place(a.token_seq, a.token_pos, t0 + tid, a.B, a.max_blocks, s, p);
+            const Window win(ok ? p : 0, a.n_sink, a.n_local);
+            s_range[t0 + tid - n0] = ok && win.candidates() > a.n_top ? make_int2(win.first, win.w0) : make_int2(0, 0);
+        }
+        for (int i = tid; i < kScoreBlocks; i += 256) {
+            const int32_t entry = i < count ? table[i] : -1;
+            s_entry[i] = entry;
+            s_exp[i] = i < count ? block_exponent(g, a, kvh, entry) : kNoBlock;
+        }
+        __syncthreads();
+        for (int row0 = 0; row0 < (kTiles > 1 ? 1 : g.G); row0 += 16) {
+            if (kTiles == 1) {
+                q[0] = rows_at(row0);
+                asm volatile("" : "+v"(q[0].scale[0]));  // (here, before the counted loads)
+            }
+            for (int k = 0; k < 2 && k < rounds; ++k) tile(k).load(g, a, kvh, s_entry[64 * k + 16 * w + r16], lane);
+            for (int k = 0; k < rounds; ++k) {
+                if (k + 1 < rounds) wait_loads<Tile::kLoads>();
+                else wait_loads<0>();
+                i32x4 b[QueryRows<kD>::kSteps];
+                tile(k).operands(b, r16, q4);
+                if (k + 2 < rounds) tile(k).load(g, a, kvh, s_entry[64 * (k + 2) + 16 * w + r16], lane);
+                const int i = 64 * k + 16 * w + r16, j = j0 + i;
+                if (kTiles == 1) {
+                    float m = column_max(row_products<kD>(q[0], b));
+                    const Window win(pos, a.n_sink, a.n_local);
+                    uint32_t *at = a.scores + ((int64_t)(t0 - a.n0) * g.Hkv + kvh) * a.score_stride + (j - win.first);
+                    if (q4 == 0 && i < count) {
+                        if (row0 > 0) m = fmaxf(m, __uint_as_float(*at));      // (of this lane's own earlier rows)
+                        *at = row0 + 16 >= g.G ? score_key(m, s_exp[i]) : __float_as_uint(m);
+                    }
+                } else {
+                    float *mine = s_prod[w];
 #pragma unroll
-        for (int s = 0; s < kSteps / 2; ++s)
+                    for (int t = 0; t < kTiles; ++t) {
+                        const f32x4 p = row_products<kD>(q[t], b);
 #pragma unroll
-            for (int c = 0; c < (kBf16 ? 2 : 4); ++c) {
-                const uint4 v = *(const uint4 *)(qr + (64 * s + 16 * q4) * (kBf16 ? 2 : 4) + c * 16);
-                const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (kBf16) {
-                        x[s][8 * c + 2 * k] = __uint_as_float(u[k] << 16);
-                        x[s][8 * c + 2 * k + 1] = __uint_as_float(u[k] & 0xffff0000u);
-                    } else {
-                        x[s][4 * c + k] = __uint_as_float(u[k]);
+                        for (int e = 0; e < 4; ++e) mine[(16 * t + 4 * q4 + e) * 17 + r16] = p[e];
+                    }
+                    // a token's block: the largest of its G rows
+                    for (int tok = t0 + q4; tok < t1; tok += 4) {
+                        const float *p = mine + (tok - n0) * g.G * 17 + r16;
+                        float m = p[0];
+                        for (int h = 1; h < g.G; ++h) m = fmaxf(m, p[17 * h]);
+                        const int2 own = s_range[tok - n0];
+                        if (i < count && j >= own.x && j < own.y)
+                            a.scores[((int64_t)(tok - a.n0) * g.Hkv + kvh) * a.score_stride + (j - own.x)] = score_key(m, s_exp[i]);
                     }
                 }
             }
-#pragma unroll
-        for (int s = 0; s < kSteps / 2; ++s)
-#pragma unroll
-            for (int k = 0; k < 16; ++k) size = max(size, __float_as_uint(x[s][k]) & 0x7fffffffu);
-        size = max(size, (uint32_t)__shfl_xor((int)size, 16));
-        size = max(size, (uint32_t)__shfl_xor((int)size, 32));
-        const bool finite = size < 0x7f800000u;
-        const int f = finite ? step_exponent(__uint_as_float(size)) : 0;
-        const float by = finite ? step_pow2(-f) : 0.f;
-        i32x4 qa[kSteps];
-#pragma unroll
-        for (int s = 0; s < kSteps / 2; ++s)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                uint32_t plus = 0, minus = 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = finite ? (int)rintf(x[s][4 * k + e] * by) : 0;
-                    plus |= (uint32_t)max(i, 0) << (8 * e);
-                    minus |= ((uint32_t)min(i, 0) & 0xffu) << (8 * e);
-                }
-                qa[s][k] = (int)plus;
-                qa[kSteps / 2 + s][k] = (int)minus;
-            }
-        // rows 4 q4 + e of the products stand in this lane: their powers of two, and whether they count
-        float scale[4];
-        bool counts[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int src = 4 * q4 + e;
-            scale[e] = step_pow2(__shfl(f, src));
-            counts[e] = row0 + src < g.G && __shfl((int)finite, src) != 0;
         }
-#pragma unroll
-        for (int i = 0; i < kScoreBlocks / 64; ++i) {
-            const int j = j0 + i * 64 + w * 16 + r16;
-            if (j0 + i * 64 + w * 16 >= win.w0) break;
-            const int32_t entry = j < win.w0 ? table[j] : -1;
-            const int bid = entry >= 0 ? entry_bid(entry) : -1;
-            const bool ok = bid >= a.first_block && bid < g.n_blocks;
-            const i32x4 *src = (const i32x4 *)(bounds + (int64_t)(ok ? bid : a.first_block) * (2 * kD) + 16 * q4);
-            i32x4 acc = {0, 0, 0, 0}, b[kSteps];
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) b[s] = src[4 * s];
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(qa[s], b[s], acc, 0, 0, 0);
-            float m = -INFINITY;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (counts[e]) m = fmaxf(m, (float)acc[e] * scale[e]);
-            best[i] = fmaxf(best[i], m);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < kScoreBlocks / 64; ++i) {
-        const int j = j0 + i * 64 + w * 16 + r16;
-        float m = best[i];
-        m = fmaxf(m, __shfl_xor(m, 16));
-        m = fmaxf(m, __shfl_xor(m, 32));
-        if (q4 != 0 || j >= win.w0) continue;
-        const int32_t entry = table[j];
-        const int bid = entry >= 0 ? entry_bid(entry) : -1;
-        if (bid >= a.first_block && bid < g.n_blocks) {
-            const int e = exps[bid];
-            m = e == 127 ? INFINITY : m * step_pow2(e) + 0.f;       // (+ 0: the two zeros are equal)
-        } else {
-            m = -INFINITY;                               // no block: last of all
-        }
-        const uint32_t u = __float_as_uint(m);
-        scores[j - win.first] = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
     }
 }
 
 // ------------------------------------------------------------------------------------ lists
+// All of a list but the chosen candidates; where all candidates are listed, those too.
+__device__ __forceinline__ void write_fixed(const SelectArgs &a, const Window &win, int32_t *list, int tid, int threads)
+{
+    const int cand = win.candidates(), n_list = a.n_sink + a.n_top + a.n_local;
+    const int n_chosen = min(cand, a.n_top), n_all = win.first + n_chosen + (win.own - win.w0 + 1);
+    for (int i = tid; i < n_list; i += threads)
+        if (i < win.first) list[i] = i;
+        else if (i >= n_all) list[i] = -1;
+        else if (i >= win.first + n_chosen) list[i] = win.w0 + (i - win.first - n_chosen);
+        else if (cand <= a.n_top) list[i] = i;
+}
+
 // The n_top best of a token's candidates and, behind ties, the lower ones; written in ascending order between the first
 // blocks and the last.  A work-group per (token, KV head).  The n_top-th largest score is found by bins over the range that
 // still holds it: a histogram of 1024 equal bins between its ends, the bin that the count falls into, and again inside that
@@ -173,12 +317,7 @@ __global__ __launch_bounds__(256) void select_kernel(Geom g, SelectArgs a)
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int cand = win.candidates(), n_list = a.n_sink + a.n_top + a.n_local;
     int32_t *list = a.lists + ((int64_t)n * g.Hkv + kvh) * n_list;
-    const int n_chosen = min(cand, a.n_top), n_all = win.first + n_chosen + (win.own - win.w0 + 1);
-    for (int i = tid; i < n_list; i += 256)
-        if (i < win.first) list[i] = i;
-        else if (i >= n_all) list[i] = -1;
-        else if (i >= win.first + n_chosen) list[i] = win.w0 + (i - win.first - n_chosen);
-        else if (cand <= a.n_top) list[i] = i;
+    write_fixed(a, win, list, tid, 256);
     if (cand <= a.n_top || a.n_top == 0) return;
     const uint32_t *scores = a.scores + ((int64_t)(n - a.n0) * g.Hkv + kvh) * a.score_stride;
     uint32_t lo = 0xffffffffu, hi = 0;
@@ -267,45 +406,217 @@ __global__ __launch_bounds__(256) void select_kernel(Geom g, SelectArgs a)
     }
 }
 
-hipError_t launch_select(const Geom &g, SelectArgs a, const Launch &L)
+// Scores and list in one launch, for few tokens whose tables are not long: a work-group of sixteen waves a (token, KV head), the
+// scores in LDS.  A CU takes its digests at some 100 GB/s, so beyond kFusedBlocks table entries a launch that spreads them over the chip
+// pays for itself (and for many tokens, one that reads them once for several).
+constexpr int kFusedBlocks = 2048, kFusedItems = 512;
+
+// The sum of the waves' values before wave w, and of all of them.
+__device__ __forceinline__ uint32_t before_wave(const uint32_t (&s_wave)[16], int w)
+{
+    uint32_t sum = 0;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) sum += k < w ? s_wave[k] : 0;
+    return sum;
+}
+
+template <bool kBf16, int kD>
+__global__ __launch_bounds__(1024) void score_select_kernel(Geom g, SelectArgs a)
+{
+    extern __shared__ __attribute__((aligned(256))) char s_ring[];       // two tiles a wave
+    __shared__ __attribute__((aligned(16))) uint32_t s_bins[kSelectBins], s_lo[16], s_hi[16], s_wave[16];
+    __shared__ int32_t s_entry[kFusedBlocks];
+    __shared__ float s_prod[kFusedBlocks];
+    __shared__ uint32_t s_found[3];
+    const int n = a.n0 + blockIdx.x / g.Hkv, kvh = blockIdx.x % g.Hkv;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, q4 = lane >> 4;
+    auto rows_at = [&](int row0) {
+        return query_rows<kBf16, kD>(a.q + ((int64_t)n * g.Hq + kvh * g.G + min(row0 + r16, g.G - 1)) * g.head_bytes, row0 + r16 < g.G, q4);
+    };
+    QueryRows<kD> q = rows_at(0);                        // (while the token's place is looked up)
+    s_bins[tid] = 0;
+    int seq, pos;
+    if (!token_place(a.token_seq, a.token_pos, n, a.B, a.max_blocks, seq, pos)) return;
+    const Window win(pos, a.n_sink, a.n_local);
+    const int cand = win.candidates(), n_list = a.n_sink + a.n_top + a.n_local;
+    int32_t *list = a.lists + ((int64_t)n * g.Hkv + kvh) * n_list;
+    if (cand <= a.n_top || a.n_top == 0) {
+        write_fixed(a, win, list, tid, 1024);
+        return;
+    }
+    const int32_t *table = a.block_table + (int64_t)seq * a.max_blocks + win.first;
+
+    // ---- scores: wave w takes blocks 16 w .. 16 w + 15 of every 256; thread t makes keys of those of candidates 2t and 2t + 1
+    typedef BoundsTile<kD> Tile;
+    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)s_ring + w * 2 * Tile::kBytes;
+    auto tile = [&](int k) { return Tile{ring + (uint32_t)(k & 1) * Tile::kBytes}; };
+    const int c0 = 2 * tid;
+    int32_t entry[2] = {-1, -1};
+    int exponent[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        if (c0 + k < cand) s_entry[c0 + k] = entry[k] = table[c0 + k];
+    __syncthreads();
+    const int rounds = cand > 16 * w ? (cand - 16 * w + 255) >> 8 : 0;
+    auto entry_of = [&](int k) { const int i = 256 * k + 16 * w + r16; return i < cand ? s_entry[i] : -1; };
+    for (int row0 = 0; row0 < g.G; row0 += 16) {
+        if (row0 > 0) q = rows_at(row0);
+        for (int k = 0; k < 2 && k < rounds; ++k) tile(k).load(g, a, kvh, entry_of(k), lane);
+        if (row0 == 0) {                                 // (needed last: behind the first bounds)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) exponent[k] = block_exponent(g, a, kvh, entry[k]);
+        }
+        for (int k = 0; k < rounds; ++k) {
+            if (k + 1 < rounds) wait_loads<Tile::kLoads>();
+            else wait_loads<0>();
+            i32x4 b[QueryRows<kD>::kSteps];
+            tile(k).operands(b, r16, q4);
+            if (k + 2 < rounds) tile(k).load(g, a, kvh, entry_of(k + 2), lane);
+            float m = column_max(row_products<kD>(q, b));
+            const int i = 256 * k + 16 * w + r16;
+            if (q4 == 0 && i < cand) {
+                if (row0 > 0) m = fmaxf(m, s_prod[i]);   // (of this wave's own earlier rows)
+                s_prod[i] = m;
+            }
+        }
+    }
+    __syncthreads();
+    uint32_t key[2] = {0, 0}, lo = 0xffffffffu, hi = 0;
+    bool have[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        have[k] = c0 + k < cand;
+        if (have[k]) {
+            key[k] = score_key(s_prod[c0 + k], exponent[k]);
+            lo = min(lo, key[k]);
+            hi = max(hi, key[k]);
+        }
+    }
+    hi = wave_max(hi);
+    lo = ~wave_max(~lo);
+    if (lane == 0) { s_lo[w] = lo; s_hi[w] = hi; }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 16; ++k) { lo = min(lo, s_lo[k]); hi = max(hi, s_hi[k]); }
+
+    // ---- the threshold, as in select_kernel; a thread holds two neighbouring candidates, and a bin
+    uint32_t want = a.n_top;
+    bool whole = false;
+    while (lo < hi) {
+        const int shift = max(0, 22 - (int)__builtin_clz(hi - lo));
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (have[k] && key[k] >= lo && key[k] <= hi) atomicAdd(&s_bins[(key[k] - lo) >> shift], 1u);
+        __syncthreads();
+        const uint32_t c = s_bins[kSelectBins - 1 - tid], x = wave_prefix(c);       // counted from the top
+        if (lane == 63) s_wave[w] = x;
+        __syncthreads();
+        s_bins[tid] = 0;
+        const uint32_t upto = before_wave(s_wave, w) + x;
+        if (upto >= want && upto - c < want) { s_found[0] = kSelectBins - 1 - tid; s_found[1] = upto - c; s_found[2] = c; }
+        __syncthreads();
+        whole = want - s_found[1] == s_found[2];         // all of the bin: its lower end is the threshold
+        want -= s_found[1];
+        lo += s_found[0] << shift;
+        hi = shift == 0 ? lo : min(hi, lo + ((1u << shift) - 1));
+        if (whole) break;
+    }
+    // ---- chosen: keys above the threshold, and the first `want` of those at it
+    bool over[2], tie[2];
+    uint32_t mine = 0;                                   // (keys at the threshold << 16) + keys above it
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        over[k] = have[k] && (whole ? key[k] >= lo : key[k] > lo);
+        tie[k] = have[k] && !whole && key[k] == lo;
+        mine += (over[k] ? 1u : 0u) + (tie[k] ? 0x10000u : 0u);
+    }
+    const uint32_t x = wave_prefix(mine);
+    if (lane == 63) s_wave[w] = x;                       // (its last reads were before the loop's last barrier)
+    __syncthreads();
+    const uint32_t before = before_wave(s_wave, w) + x - mine;
+    uint32_t above = before & 0xffffu, ties = before >> 16;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        if (over[k] || (tie[k] && ties < want)) list[win.first + above + min(ties, want)] = win.first + c0 + k;
+        above += over[k];
+        ties += tie[k];
+    }
+    write_fixed(a, win, list, tid, 1024);                // (last: a barrier behind a store to memory waits for it)
+}
+
+template <bool kBf16, int kD>
+static hipError_t launch_score_select(const Geom &g, const SelectArgs &a, const Launch &L)
+{
+    constexpr int kLds = 16 * 2 * BoundsTile<kD>::kBytes;
+    static PerDeviceOnce configured;
+    const hipError_t e = configured.run([] {
+        return hipFuncSetAttribute((const void *)score_select_kernel<kBf16, kD>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    });
+    if (e != hipSuccess) return e;
+    TC_LAUNCH_N((score_select_kernel<kBf16, kD>), a.n_tokens * g.Hkv, 1024, kLds, L, g, a);
+    return hipGetLastError();
+}
+
+template <bool kBf16, int kD>
+static hipError_t launch_scores(const Geom &g, SelectArgs a, const Launch &L)
+{
+    // several tokens a work-group where requests bring more than one each
+    const bool grouped = a.n_tokens > a.B && g.G <= 32;
+    a.group_tokens = grouped ? 64 / g.G : 1;
+    a.score_parts = (a.max_blocks + kScoreBlocks - 1) / kScoreBlocks;
+    const int64_t grid = (int64_t)((a.n_tokens + a.group_tokens - 1) / a.group_tokens) * g.Hkv * a.score_parts;
+    if (grid > INT32_MAX) return hipErrorInvalidValue;
+    if (grouped) TC_LAUNCH((score_kernel<kBf16, kD, 4>), (unsigned)grid, 0, L, g, a);
+    else TC_LAUNCH((score_kernel<kBf16, kD, 1>), (unsigned)grid, 0, L, g, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_select(const Geom &g, const SelectArgs &a, const Launch &L)
 {
     if (a.n_tokens == 0) return hipSuccess;
     const int most = a.max_blocks;                       // candidates of any token
-    a.score_parts = (most + kScoreBlocks - 1) / kScoreBlocks;
-    const int64_t grid64 = (int64_t)a.n_tokens * g.Hkv * std::max(a.score_parts, 1);
-    if (grid64 > INT32_MAX) return hipErrorInvalidValue;
-    const unsigned grid = (unsigned)grid64;
+    const int64_t items = (int64_t)a.n_tokens * g.Hkv;
+    if (items > INT32_MAX) return hipErrorInvalidValue;
+    if (most <= kFusedBlocks && items <= kFusedItems)
+        return g.esize == 2 ? launch_score_select<true, 128>(g, a, L)
+             : g.D == 64 ? launch_score_select<false, 64>(g, a, L) : launch_score_select<false, 128>(g, a, L);
     if (most > a.n_top && a.n_top > 0) {
-        if (g.esize == 2) TC_LAUNCH((score_kernel<true, 128>), grid, 0, L, g, a);
-        else if (g.D == 64) TC_LAUNCH((score_kernel<false, 64>), grid, 0, L, g, a);
-        else TC_LAUNCH((score_kernel<false, 128>), grid, 0, L, g, a);
+        const hipError_t e = g.esize == 2 ? launch_scores<true, 128>(g, a, L)
+                           : g.D == 64 ? launch_scores<false, 64>(g, a, L) : launch_scores<false, 128>(g, a, L);
+        if (e != hipSuccess) return e;
     }
     static PerDeviceOnce configured;
     const hipError_t e = configured.run([] {
         return hipFuncSetAttribute((const void *)select_kernel<true>, hipFuncAttributeMaxDynamicSharedMemorySize, kSelectLds * 4);
     });
     if (e != hipSuccess) return e;
-    if (most <= kSelectLds) TC_LAUNCH(select_kernel<true>, a.n_tokens * g.Hkv, most * 4, L, g, a);
-    else TC_LAUNCH(select_kernel<false>, a.n_tokens * g.Hkv, 0, L, g, a);
+    if (most <= kSelectLds) TC_LAUNCH(select_kernel<true>, (unsigned)items, most * 4, L, g, a);
+    else TC_LAUNCH(select_kernel<false>, (unsigned)items, 0, L, g, a);
     return hipGetLastError();
 }
 
 // ------------------------------------------------------------------------------------ attention
+__device__ __forceinline__ void write_bf16x4(char *dst, f32x4 x)
+{
+    uint32_t r[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        r[k] = (uint32_t)__builtin_bit_cast(unsigned short, (__bf16)x[2 * k]) | ((uint32_t)__builtin_bit_cast(unsigned short, (__bf16)x[2 * k + 1]) << 16);
+    *(uint2 *)dst = make_uint2(r[0], r[1]);
+}
+
 // out = softmax(sm_scale q . k) v over the keys of the listed blocks at positions up to the token's own that hold a token;
 // zeros where there are none.  A token and KV head have G rows that share a list, so as in the decode kernel the work is
 // reading the listed keys and values once, and a short list is a chain of round trips.
 //
-// A work-group is (token, KV head, 16 rows, range of the list); its four waves take the range's units in turn, keep their own
-// running maximum and sum, and are combined through LDS at the end.  K and V go straight from memory into the registers that
-// the matrix instructions read: a wave's lists are short, 16 KB of loads are in flight from one unit, and no wave waits for
-// another before the end.
+// A work-group is (token, KV head, 16 rows, range of the list); its waves take the range's units in turn, keep their own
+// running maximum and sum, and are combined through LDS at the end.  No wave waits for another before that.
 struct ListUnit { int32_t j, entry; int valid; };
 
-// Block `i` of the list: its logical number, its table entry and how many of its positions the token sees (0: none).
-__device__ __forceinline__ ListUnit list_unit(const Geom &g, const BlockAttnArgs &a, const int32_t *list, const int32_t *table, int i, int end, int pos)
+// Block j of a list: its table entry and how many of its positions the token sees (0: none).
+__device__ __forceinline__ ListUnit list_unit(const Geom &g, const BlockAttnArgs &a, int32_t j, const int32_t *table, int pos)
 {
-    ListUnit u{-1, -1, 0};
-    if (i < end) u.j = list[i];
+    ListUnit u{j, -1, 0};
     if (u.j >= 0 && u.j <= pos >> 4) u.entry = table[u.j];
     const int bid = entry_bid(u.entry);
     if (u.entry >= 0 && bid >= a.first_block && bid < g.n_blocks) u.valid = min(kBlockTokens - entry_pad(u.entry), pos - u.j * kBlockTokens + 1);
@@ -317,27 +628,43 @@ __device__ __forceinline__ ListUnit list_unit(const Geom &g, const BlockAttnArgs
 // half q4 % 2) belong to the eight tokens whose values stand in one 16-byte piece of the pool's V rows, and O^T += V^T P^T
 // takes both as they are.  Weights are rounded to bf16 for that product (as in every attention kernel here; their sum is of
 // the fp32 ones).  Values at positions that the token does not see are replaced by zeros, whatever stands there.
-constexpr int kBaRow = 132;
+//
+// A unit's 16 KB come by direct loads into the wave's own piece of LDS, a kilobyte of neighbouring bytes each, and the operands
+// from there: loaded straight into the operands' registers, where neighbouring lanes are neighbouring rows of 256 bytes, keys take a
+// CU's address path 64 cycles a kilobyte instead of 16.  The next unit's keys are requested as soon as this one's are in
+// registers, and so the values.  (Values straight to registers, 32-byte rows, and twice the waves: slower for every list tried.)
+constexpr int kBaRow = 132;                              // padded output row of the exchange (floats), maximum and sum behind it
+constexpr int kBaBlock = 4096;                           // one head's K (or V) in one block
+constexpr int kBaWave = 4 * kBaBlock;                    // K of a unit: rows of 256 bytes, 16-byte chunk c of row r at c ^ r; V: two blocks verbatim
 
-template <bool kSplit>
-__global__ __launch_bounds__(256, 2) void block_attn_bf16_kernel(Geom g, BlockAttnArgs a)
+constexpr float kBaRescale = 8.f;                        // weights grow to 2^8 before the reference moves
+
+template <int kWaves, bool kSplit>
+__global__ __launch_bounds__(64 * kWaves, 2) void block_attn_bf16_kernel(Geom g, BlockAttnArgs a)
 {
-    __shared__ __attribute__((aligned(16))) float s_o[4][16 * kBaRow];
-    __shared__ float s_ml[4][16][2];
+    extern __shared__ __attribute__((aligned(16))) char lds_raw[];
     const int chunks = (g.G + 15) >> 4;
     const int item = blockIdx.x / a.n_splits, split = blockIdx.x - item * a.n_splits;
     const int n = item / (g.Hkv * chunks), hc = item - n * (g.Hkv * chunks), kvh = hc / chunks, row0 = (hc - kvh * chunks) * 16;
-    int seq, pos;
-    if (!token_place(a.token_seq, a.token_pos, n, a.B, a.max_blocks, seq, pos)) return;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, q4 = lane >> 4;
     const int rows = min(16, g.G - row0);
     const int32_t *list = a.lists + ((int64_t)n * g.Hkv + kvh) * a.n_list;
-    const int32_t *table = a.block_table + (int64_t)seq * a.max_blocks;
     const int n_units = (a.n_list + 1) >> 1;
     const int u0 = (int)((int64_t)n_units * split / a.n_splits), u1 = (int)((int64_t)n_units * (split + 1) / a.n_splits);
     const int end = min(2 * u1, a.n_list);
-    const char *pool = g.pool + (int64_t)a.layer * g.layer_stride + (int64_t)kvh * (kBlockTokens * 256);
+    // a wave's units 32 at a time: lane 2k + b looks up block b of unit k
+    auto listed = [&](int k0) { const int i = 2 * (k0 + kWaves * (lane >> 1)) + (lane & 1); return i < end ? list[i] : -1; };
+    int32_t j_next = listed(u0 + w);                     // (while the token's place is looked up)
+    int seq, pos;
+    if (!token_place(a.token_seq, a.token_pos, n, a.B, a.max_blocks, seq, pos)) return;
+    const int32_t *table = a.block_table + (int64_t)seq * a.max_blocks;
+    const char *pool = g.pool + (int64_t)a.layer * g.layer_stride + (int64_t)kvh * kBaBlock;
     const int64_t v_half = g.block_bytes >> 1;
+    // the XOR addressing of the K rows needs them 256-byte aligned
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds_raw, slack = (256u - (lds_base & 255u)) & 255u;
+    char *lds = lds_raw + slack;
+    const uint32_t lds_w = lds_base + slack + w * kBaWave;
+    typedef const __attribute__((address_space(3))) bf16x8 *lds_frag;
 
     bf16x8 qf[4];
     {
@@ -350,30 +677,53 @@ __global__ __launch_bounds__(256, 2) void block_attn_bf16_kernel(Geom g, BlockAt
     for (int db = 0; db < 8; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m_run = -INFINITY, l_lane = 0.f;
 
-    const uint32_t k_off = (uint32_t)(r16 & 7) * 256 + q4 * 16, v_off = (uint32_t)r16 * 32 + (q4 & 1) * 16;
-    // a wave's units 32 at a time: lane 2k + b looks up block b of unit k
-    for (int k0 = u0 + w; k0 < u1; k0 += 4 * 32) {
-        const ListUnit mine = list_unit(g, a, list, table, 2 * (k0 + 4 * (lane >> 1)) + (lane & 1), end, pos);
-        const int n_mine = min(32, (u1 - k0 + 3) >> 2);
-        bf16x8 kf[8], vf[8];
-        int valid0 = 0, valid1 = 0;
-        auto fetch = [&](int k, int &v0, int &v1) {      // a unit whose blocks are both empty loads nothing
-            v0 = __builtin_amdgcn_readlane(mine.valid, 2 * k);
-            v1 = __builtin_amdgcn_readlane(mine.valid, 2 * k + 1);
-            if (v0 <= 0 && v1 <= 0) return;
-            int b0 = entry_bid(__builtin_amdgcn_readlane(mine.entry, 2 * k)), b1 = entry_bid(__builtin_amdgcn_readlane(mine.entry, 2 * k + 1));
-            if (v0 <= 0) b0 = b1;                        // (what is loaded in an empty block's place is masked)
-            if (v1 <= 0) b1 = b0;
-            const char *p0 = pool + (int64_t)b0 * g.block_bytes, *p1 = pool + (int64_t)b1 * g.block_bytes;
-            const char *kp = (r16 < 8 ? p0 : p1) + k_off, *vp = (q4 < 2 ? p0 : p1) + v_half + v_off;
+    uint32_t k_off[4], v_off[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) kf[i] = *(const bf16x8 *)(kp + (i >> 2) * 2048 + (i & 3) * 64);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) vf[i] = *(const bf16x8 *)(vp + i * 512);
+    for (int i = 0; i < 4; ++i) {
+        k_off[i] = (uint32_t)((lane >> 4) * 256 + (((lane & 15) ^ (4 * i + (lane >> 4))) * 16));
+        v_off[i] = (uint32_t)lane * 16;
+    }
+    // the operands of this lane: K row r16 & 7 (+ 8) of block r16 / 8, chunk 4 ks + q4; V row 16 db + r16 of block q4 / 2, half q4 & 1
+    const uint32_t kr = (uint32_t)(r16 & 7), kb = lds_w + (r16 >> 3) * kBaBlock + kr * 256 + ((q4 ^ kr) << 4);
+    const uint32_t vb = lds_w + 2 * kBaBlock + (q4 >> 1) * kBaBlock + r16 * 32 + (q4 & 1) * 16;
+
+    for (int k0 = u0 + w; k0 < u1; k0 += kWaves * 32) {
+        const ListUnit mine = list_unit(g, a, j_next, table, pos);
+        j_next = listed(k0 + kWaves * 32);
+        const uint64_t some = __ballot(mine.valid > 0);
+        if (some == 0) continue;
+        const int n_mine = (65 - __builtin_clzll(some)) >> 1;        // up to the last unit with a key
+        asm volatile("" : "+v"(qf[0]), "+v"(qf[1]), "+v"(qf[2]), "+v"(qf[3]));      // (in registers: nothing but the counted loads is outstanding from here on)
+        auto sources = [&](int k, const char *(&src)[2]) {
+            const int v0 = __builtin_amdgcn_readlane(mine.valid, 2 * k), v1 = __builtin_amdgcn_readlane(mine.valid, 2 * k + 1);
+            const int b0 = entry_bid(__builtin_amdgcn_readlane(mine.entry, 2 * k)), b1 = entry_bid(__builtin_amdgcn_readlane(mine.entry, 2 * k + 1));
+            // (what is loaded in an empty block's place is masked)
+            src[0] = pool + (int64_t)(v0 > 0 ? b0 : v1 > 0 ? b1 : a.first_block) * g.block_bytes;
+            src[1] = pool + (int64_t)(v1 > 0 ? b1 : v0 > 0 ? b0 : a.first_block) * g.block_bytes;
         };
+        auto issue_k = [&](const char *const (&src)[2]) {
+            load4_to_lds(lds_w, src[0], k_off);
+            load4_to_lds(lds_w + kBaBlock, src[1], k_off);
+        };
+        auto issue_v = [&](const char *const (&src)[2]) {
+            load4_to_lds(lds_w + 2 * kBaBlock, src[0] + v_half, v_off);
+            load4_to_lds(lds_w + 3 * kBaBlock, src[1] + v_half, v_off);
+        };
+        const char *src[2];
+        sources(0, src);
+        issue_k(src);
+        issue_v(src);
         for (int k = 0; k < n_mine; ++k) {
-            fetch(k, valid0, valid1);
-            if (valid0 <= 0 && valid1 <= 0) continue;
+            const bool more = k + 1 < n_mine;
+            wait_loads<8>();                             // K is there, V may be on its way
+            bf16x8 kf[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) kf[i] = *(lds_frag)(uintptr_t)(((kb ^ ((i & 3) << 6)) ^ ((i >> 2) << 7)) + (i >> 2) * 2048);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // K area read out
+            if (more) {
+                sources(k + 1, src);
+                issue_k(src);
+            }
             f32x4 s[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -381,6 +731,14 @@ __global__ __launch_bounds__(256, 2) void block_attn_bf16_kernel(Geom g, BlockAt
 #pragma unroll
                 for (int ks = 0; ks < 4; ++ks) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[4 * h + ks], qf[ks], s[h], 0, 0, 0);
             }
+            if (more) wait_loads<8>();
+            else wait_loads<0>();
+            bf16x8 vf[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) vf[i] = *(lds_frag)(uintptr_t)(vb + i * 512);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // V area read out
+            if (more) issue_v(src);
+            const int valid0 = __builtin_amdgcn_readlane(mine.valid, 2 * k), valid1 = __builtin_amdgcn_readlane(mine.valid, 2 * k + 1);
             if (valid0 < kBlockTokens || valid1 < kBlockTokens) {
                 const int seen = (q4 < 2 ? valid0 : valid1) - 4 * (q4 & 1);      // of this lane's tokens 0..3 and 8..11
 #pragma unroll
@@ -394,10 +752,9 @@ __global__ __launch_bounds__(256, 2) void block_attn_bf16_kernel(Geom g, BlockAt
                     }
             }
             float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-            mx = fmaxf(mx, __shfl_xor(mx, 16));
-            mx = fmaxf(mx, __shfl_xor(mx, 32));
-            const float m_new = fmaxf(m_run, mx * a.scale_log2);
-            if (__any(m_new > m_run)) {
+            const float mxs = max_of_quarters(mx) * a.scale_log2;
+            if (__any(mxs > m_run + kBaRescale)) {       // also taken while m_run is still -inf
+                const float m_new = fmaxf(m_run, mxs);
                 const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
                 l_lane *= alpha;
 #pragma unroll
@@ -421,41 +778,37 @@ __global__ __launch_bounds__(256, 2) void block_attn_bf16_kernel(Geom g, BlockAt
         }
     }
 
-    // the waves' (maximum, sum, output) rows, combined by 16 threads a row, eight columns each
+    // the waves' (output, maximum, sum) rows, combined by 32 threads a row, four columns each
     float l_row = l_lane + __shfl_xor(l_lane, 16);
     l_row += __shfl_xor(l_row, 32);
+    if (r16 < rows) {
+        float *mine = (float *)(lds + w * kBaWave) + r16 * kBaRow;
 #pragma unroll
-    for (int db = 0; db < 8; ++db) *(f32x4 *)&s_o[w][r16 * kBaRow + 16 * db + 4 * q4] = o[db];
-    if (q4 == 0) { s_ml[w][r16][0] = m_run; s_ml[w][r16][1] = l_row; }
-    __syncthreads();
-    const int row = tid >> 4, d = 8 * (tid & 15);
-    if (row >= rows) return;
-    float M = -INFINITY, sum = 0.f, acc[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) M = fmaxf(M, s_ml[k][row][0]);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const float mk = s_ml[k][row][0];
-        // (no maximum: no keys - its sums are zeros - or only scores that are NaN, and so are they)
-        const float wgt = mk == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mk - M);
-        sum += wgt * s_ml[k][row][1];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += wgt * s_o[k][row * kBaRow + d + e];
+        for (int db = 0; db < 8; ++db) *(f32x4 *)(mine + 16 * db + 4 * q4) = o[db];
+        if (q4 == 0) *(float2 *)(mine + 128) = make_float2(m_run, l_row);
     }
-    const int64_t out_row = (int64_t)n * g.Hq + kvh * g.G + row0 + row;
-    if (kSplit) {
-        float *po = a.part_o + (out_row * a.n_splits + split) * 128 + d;
-        *(f32x4 *)po = f32x4{acc[0], acc[1], acc[2], acc[3]};
-        *(f32x4 *)(po + 4) = f32x4{acc[4], acc[5], acc[6], acc[7]};
-        if (d == 0) *(float2 *)(a.part_ml + (out_row * a.n_splits + split) * 2) = make_float2(M, sum);
-    } else {
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        bf16x8 y;
+    __syncthreads();
+    const int d = 4 * (tid & 31);
+    for (int row = tid >> 5; row < rows; row += 2 * kWaves) {
+        RowSum x{-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = (__bf16)(acc[e] * inv);
-        *(bf16x8 *)(a.out + out_row * 256 + d * 2) = y;
+        for (int k = 0; k < kWaves; ++k) x.M = fmaxf(x.M, ((const float *)(lds + k * kBaWave))[row * kBaRow + 128]);
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) {
+            const float *other = (const float *)(lds + k * kBaWave) + row * kBaRow;
+            const float2 ml = *(const float2 *)(other + 128);
+            // (no maximum: no keys - its sums are zeros - or only scores that are NaN, and so are they)
+            const float wgt = ml.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml.x - x.M);
+            x.L += wgt * ml.y;
+            x.acc += wgt * *(const f32x4 *)(other + d);
+        }
+        const int64_t out_row = (int64_t)n * g.Hq + kvh * g.G + row0 + row;
+        if (kSplit) {
+            *(f32x4 *)(a.part_o + (out_row * a.n_splits + split) * 128 + d) = x.acc;
+            if (d == 0) *(float2 *)(a.part_ml + (out_row * a.n_splits + split) * 2) = make_float2(x.M, x.L);
+        } else {
+            write_bf16x4(a.out + out_row * 256 + d * 2, x.acc * (x.L == 0.f ? 0.f : 1.f / x.L));
+        }
     }
 }
 
@@ -489,7 +842,7 @@ __global__ __launch_bounds__(256, 2) void block_attn_f32_kernel(Geom g, BlockAtt
         l_run[r] = 0.f;
     }
     for (int k0 = u0 + w; k0 < u1; k0 += 4 * 64) {
-        const ListUnit mine = list_unit(g, a, list, table, k0 + 4 * lane, u1, pos);
+        const ListUnit mine = list_unit(g, a, k0 + 4 * lane < u1 ? list[k0 + 4 * lane] : -1, table, pos);
         const int n_mine = min(64, (u1 - k0 + 3) >> 2);
         for (int k = 0; k < n_mine; ++k) {
             const int valid = __builtin_amdgcn_readlane(mine.valid, k);
@@ -565,29 +918,62 @@ __global__ __launch_bounds__(256) void block_merge_kernel(Geom g, BlockAttnArgs 
     int seq, pos;
     if (!token_place(a.token_seq, a.token_pos, (int)(row / g.Hq), a.B, a.max_blocks, seq, pos)) return;
     RowSum x{-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
-    for (int s = 0; s < a.n_splits; ++s) {
-        const float2 ml = *(const float2 *)(a.part_ml + (row * a.n_splits + s) * 2);
-        x.add(ml.x, ml.y, *(const f32x4 *)(a.part_o + (row * a.n_splits + s) * kD + d));
+    constexpr int kBatch = 8;                            // partials requested before the first is used
+    for (int s0 = 0; s0 < a.n_splits; s0 += kBatch) {
+        float2 ml[kBatch];
+        f32x4 po[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int64_t at = row * a.n_splits + min(s0 + j, a.n_splits - 1);
+            ml[j] = *(const float2 *)(a.part_ml + at * 2);
+            po[j] = *(const f32x4 *)(a.part_o + at * kD + d);
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            if (s0 + j < a.n_splits) x.add(ml[j].x, ml[j].y, po[j]);
     }
     const float inv = x.L == 0.f ? 0.f : 1.f / x.L;
     if (kBf16) {
-        unsigned short r[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) r[e] = __builtin_bit_cast(unsigned short, (__bf16)(x.acc[e] * inv));
-        *(uint2 *)(a.out + (row * kD + d) * 2) = make_uint2(r[0] | ((uint32_t)r[1] << 16), r[2] | ((uint32_t)r[3] << 16));
+        write_bf16x4(a.out + (row * kD + d) * 2, x.acc * inv);
     } else {
         *(f32x4 *)(a.out + (row * kD + d) * 4) = x.acc * inv;
     }
 }
 
-// As many ranges as give the chip about two work-groups a CU, none shorter than four units (one for each wave).
-int block_attn_splits(int Hq, int Hkv, int esize, int n_tokens, int n_list)
+// Waves of a work-group and ranges of a list.
+constexpr int kBaRounds = 6;
+
+struct BaShape { int waves, splits; };
+static BaShape block_attn_shape(int Hq, int Hkv, int esize, int n_tokens, int n_list)
 {
     const int G = Hq / Hkv, rows = esize == 2 ? 16 : 8;
     const int64_t items = (int64_t)n_tokens * Hkv * ((G + rows - 1) / rows);
     const int units = esize == 2 ? (n_list + 1) / 2 : n_list;
-    const int64_t want = items > 0 ? 512 / items : 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, (units + 3) / 4), 32));
+    if (esize != 2) {
+        const int64_t want = items > 0 ? 512 / items : 1;
+        return BaShape{4, (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, (units + 3) / 4), 32))};
+    }
+    if (items > 256 || units <= 4) return BaShape{4, 1};
+    if (units <= 8 * kBaRounds || items > 128) return BaShape{8, 1};
+    return BaShape{8, (int)std::min<int64_t>(std::min<int64_t>((units + 15) / 16, 256 / items), 32)};
+}
+
+int block_attn_splits(int Hq, int Hkv, int esize, int n_tokens, int n_list)
+{
+    return block_attn_shape(Hq, Hkv, esize, n_tokens, n_list).splits;
+}
+
+template <int kWaves, bool kSplit>
+static hipError_t launch_attn_bf16_waves(const Geom &g, const BlockAttnArgs &a, unsigned grid, const Launch &L)
+{
+    static PerDeviceOnce configured;
+    const hipError_t e = configured.run([] {
+        return hipFuncSetAttribute((const void *)block_attn_bf16_kernel<kWaves, kSplit>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                   kWaves * kBaWave + 256);
+    });
+    if (e != hipSuccess) return e;
+    TC_LAUNCH_N((block_attn_bf16_kernel<kWaves, kSplit>), grid, 64 * kWaves, kWaves * kBaWave + 256, L, g, a);      // (+ alignment slack)
+    return hipGetLastError();
 }
 
 hipError_t launch_block_attn(const Geom &g, const BlockAttnArgs &a, const Launch &L)
@@ -598,8 +984,9 @@ hipError_t launch_block_attn(const Geom &g, const BlockAttnArgs &a, const Launch
     if (grid > INT32_MAX) return hipErrorInvalidValue;
     const bool split = a.n_splits > 1;
     if (g.esize == 2) {
-        if (split) TC_LAUNCH(block_attn_bf16_kernel<true>, (unsigned)grid, 0, L, g, a);
-        else TC_LAUNCH(block_attn_bf16_kernel<false>, (unsigned)grid, 0, L, g, a);
+        const int waves = block_attn_shape(g.Hq, g.Hkv, g.esize, a.n_tokens, a.n_list).waves;
+        return split ? launch_attn_bf16_waves<8, true>(g, a, (unsigned)grid, L)
+             : waves == 8 ? launch_attn_bf16_waves<8, false>(g, a, (unsigned)grid, L) : launch_attn_bf16_waves<4, false>(g, a, (unsigned)grid, L);
     } else if (g.D == 64) {
         if (split) TC_LAUNCH((block_attn_f32_kernel<64, true>), (unsigned)grid, 0, L, g, a);
         else TC_LAUNCH((block_attn_f32_kernel<64, false>), (unsigned)grid, 0, L, g, a);

@@ -51,7 +51,7 @@ struct SelectArgs {
     uint32_t *scores;                         // [tokens of a round][Hkv][score_stride], ordered like the scores
     int64_t score_stride;
     int32_t n0, n_tokens, layer, B, max_blocks, n_sink, n_top, n_local, first_block;    // tokens n0 .. n0 + n_tokens - 1
-    int32_t score_parts;                      // work-groups of a (token, KV head)'s scores
+    int32_t score_parts, group_tokens;        // scores: work-groups along the candidates, and tokens of one
 };
 
 struct BlockAttnArgs {
@@ -62,6 +62,32 @@ struct BlockAttnArgs {
     float scale_log2;
     int32_t n_tokens, layer, B, max_blocks, n_list, n_splits, first_block;
 };
+
+// Over a wave's 64 lanes by DPP (a shuffle through LDS takes five times as long): inclusive prefix sums, and the largest.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ uint32_t dpp_or_zero(uint32_t x)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, kRows, 0xf, false);
+}
+__device__ __forceinline__ uint32_t wave_prefix(uint32_t x)
+{
+    x += dpp_or_zero<0x111, 0xf>(x);          // from 1, 2, 4, 8 lanes before, in each row of 16
+    x += dpp_or_zero<0x112, 0xf>(x);
+    x += dpp_or_zero<0x114, 0xf>(x);
+    x += dpp_or_zero<0x118, 0xf>(x);
+    x += dpp_or_zero<0x142, 0xa>(x);          // row 0's last lane to row 1, row 2's to row 3
+    return x + dpp_or_zero<0x143, 0xc>(x);    // lane 31 to rows 2 and 3
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t x)
+{
+    x = max(x, dpp_or_zero<0x111, 0xf>(x));
+    x = max(x, dpp_or_zero<0x112, 0xf>(x));
+    x = max(x, dpp_or_zero<0x114, 0xf>(x));
+    x = max(x, dpp_or_zero<0x118, 0xf>(x));
+    x = max(x, dpp_or_zero<0x142, 0xa>(x));
+    x = max(x, dpp_or_zero<0x143, 0xc>(x));
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
 
 // 2^e, -126 <= e <= 127
 __device__ __forceinline__ float step_pow2(int e) { return __int_as_float((e + 127) << 23); }
@@ -109,7 +135,7 @@ int block_attn_splits(int Hq, int Hkv, int esize, int n_tokens, int n_list);
 hipError_t launch_step_tables(const StepTables &s, const Launch &L);
 hipError_t launch_rope_append(const Geom &g, const RopeFreq &f, const RopeAppend &a, const Launch &L);
 hipError_t launch_digest(const Geom &g, const DigestArgs &a, int l1, const Launch &L);
-hipError_t launch_select(const Geom &g, SelectArgs a, const Launch &L);
+hipError_t launch_select(const Geom &g, const SelectArgs &a, const Launch &L);
 hipError_t launch_block_attn(const Geom &g, const BlockAttnArgs &a, const Launch &L);
 hipError_t launch_block_merge(const Geom &g, const BlockAttnArgs &a, const Launch &L);
 
