@@ -21,16 +21,15 @@ struct StepTables {
     int32_t B, max_blocks, n_spare, n_tokens, first_seq, n_blocks;
 };
 
-// Revolutions of pair j per position step, theta^(-2j/D) / (2 pi).  Must be a kernel's first argument: the
-// kernel reads it at the start of its argument segment, by a lane's own index.
-struct RopeFreq { double rev[64]; };
-
 struct RopeAppend {
     const char *q, *k, *v;                    // rows [n_tokens], the heads of a row behind one another
     int64_t q_stride, k_stride, v_stride;     // bytes from row to row
     char *q_out;
     const int32_t *pos;                       // [axes][n_tokens]
     const int64_t *slot_map;
+    // revolutions of pair j = 8 a + b per position step, theta^(-2j/D) / (2 pi), as the product of [a] and [b] (a power and a rounding
+    // off in fp64: a turn of 2^28 positions is off by 1e-8)
+    double rev_coarse[8], rev_fine[8];
     int32_t section_end[kRopeMaxAxes];        // one past the last pair of each axis
     int32_t n_tokens, layer;
 };
@@ -133,7 +132,7 @@ __device__ __forceinline__ void turn_chunk(uint4 &x, uint4 &y, const float2 *w)
 int block_attn_splits(int Hq, int Hkv, int esize, int n_tokens, int n_list);
 
 hipError_t launch_step_tables(const StepTables &s, const Launch &L);
-hipError_t launch_rope_append(const Geom &g, const RopeFreq &f, const RopeAppend &a, const Launch &L);
+hipError_t launch_rope_append(const Geom &g, const RopeAppend &a, const Launch &L);
 hipError_t launch_digest(const Geom &g, const DigestArgs &a, int l1, const Launch &L);
 hipError_t launch_select(const Geom &g, const SelectArgs &a, const Launch &L);
 hipError_t launch_block_attn(const Geom &g, const BlockAttnArgs &a, const Launch &L);

@@ -154,13 +154,29 @@ hipError_t launch_step_tables(const StepTables &s, const Launch &L)
 // re-encoding stitch the turn is a fraction of a revolution taken in fp64, sine and cosine and the rotation are fp32 and the
 // result is rounded once.
 //
-// A work-group a token: its (cos, sin) table in LDS, then a thread for every pair of 16-byte chunks.
+// A work-group a token: its (cos, sin) table in LDS, then a thread for every pair of 16-byte chunks.  The values of a bf16 block are
+// stored transposed, two bytes of a token in each row of 32; tokens that go to the same block therefore share its KV heads
+// out among their work-groups, each of which takes those heads' rows of all of them and writes whole rows (2048 tokens, 32 / 8
+// heads: 21.8 us with two-byte stores).
+struct Run { int first, len; };                          // the step's tokens of one block
+
+// The tokens around token n (slot `slot`) that stand behind one another in the same block: one load for the wave.
+__device__ __forceinline__ Run run_of(const RopeAppend &a, int n, int64_t slot, int lane)
+{
+    const int m = n + lane - 15;
+    const bool near = lane < 31 && m >= 0 && m < a.n_tokens;
+    const int64_t other = near ? a.slot_map[m] : -1, want = slot + (lane - 15);
+    const uint32_t same = (uint32_t)__ballot(near && other == want && (want >> 4) == (slot >> 4));
+    const uint32_t before = ~same & 0x7fffu, behind = ~(same >> 16) & 0x7fffu;       // the nearest that does not belong
+    const int left = before ? 14 - (31 - __builtin_clz(before)) : 15, right = behind ? __builtin_ctz(behind) : 15;
+    return Run{n - left, left + 1 + right};
+}
+
 template <bool kBf16>
-__global__ __launch_bounds__(256) void rope_append_kernel(RopeFreq, Geom g, RopeAppend a)
+__global__ __launch_bounds__(256) void rope_append_kernel(Geom g, RopeAppend a)
 {
     __shared__ float2 cs[64];
-    typedef const __attribute__((address_space(4))) double *const_doubles;
-    const const_doubles rev = (const_doubles)__builtin_amdgcn_kernarg_segment_ptr();
+    __shared__ uint4 s_v[kBf16 ? kBlockTokens * 17 : 1];  // one head's values, rows of 17 chunks
     const int tid = threadIdx.x, n = blockIdx.x;
     const int64_t slot = a.slot_map[n];
     const int64_t blk = slot >> 4;
@@ -170,7 +186,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeFreq, Geom g, Rope
     if (tid < half_d) {
         int axis = 0;
         while (tid >= a.section_end[axis]) ++axis;
-        const double turns = (double)a.pos[(int64_t)axis * a.n_tokens + n] * rev[tid];
+        const double turns = (double)a.pos[(int64_t)axis * a.n_tokens + n] * (a.rev_coarse[tid >> 3] * a.rev_fine[tid & 7]);
         const float frac = (float)(turns - floor(turns));
         float sn, c;
         if (kBf16) {
@@ -181,17 +197,14 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeFreq, Geom g, Rope
         }
         cs[tid] = make_float2(c, sn);
     }
-    // a block that gets its first token here is zero behind the step's last token in it
-    int zero_to = t;
-    if (t == 0) {
-        zero_to = 16;
-        while (zero_to > 1 && !(n + zero_to - 1 < a.n_tokens && a.slot_map[n + zero_to - 1] == slot + zero_to - 1)) --zero_to;
-    }
-    __syncthreads();
+    const Run run = run_of(a, n, slot, tid & 63);
+    const int t_run = t - (n - run.first);               // the run's first position; 0: the block begins here, and is zero behind the run
     char *kd = g.pool + (int64_t)a.layer * g.layer_stride + blk * g.block_bytes;
     char *vd = kd + (g.block_bytes >> 1);
     constexpr int kElems = kBf16 ? 8 : 4;
-    const int rot_units = (g.Hq + g.Hkv) * half_c, units = rot_units + g.Hkv * cph;
+    const bool by_run = kBf16 && t_run == 0;
+    __syncthreads();
+    const int rot_units = (g.Hq + g.Hkv) * half_c, units = rot_units + (by_run ? 0 : g.Hkv * cph);
     for (int u = tid; u < units; u += 256) {
         if (u < rot_units) {
             const int h = u / half_c, cc = u - h * half_c;
@@ -199,8 +212,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeFreq, Geom g, Rope
             const char *src = (is_q ? a.q + n * a.q_stride + (int64_t)h * g.head_bytes : a.k + n * a.k_stride + (int64_t)(h - g.Hq) * g.head_bytes) + (cc << 4);
             char *dst = (is_q ? a.q_out + ((int64_t)n * g.Hq + h) * g.head_bytes : kd + (int64_t)((h - g.Hq) * kBlockTokens + t) * g.head_bytes) + (cc << 4);
             uint4 x = *(const uint4 *)src, y = *(const uint4 *)(src + (half_c << 4));
-            const float2 *w = cs + cc * kElems;
-            turn_chunk<kBf16>(x, y, w);
+            turn_chunk<kBf16>(x, y, cs + cc * kElems);
             *(uint4 *)dst = x;
             *(uint4 *)(dst + (half_c << 4)) = y;
         } else {
@@ -217,28 +229,42 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeFreq, Geom g, Rope
             }
         }
     }
-    if (t == 0 && zero_to < kBlockTokens) {
-        const uint4 zero = make_uint4(0, 0, 0, 0);
-        const int rows = kBlockTokens - zero_to, cpr = g.row_bytes >> 4;
-        for (int c = tid; c < rows * cpr; c += 256) {
-            const int tt = zero_to + c / cpr, w = c % cpr, h = w / cph, cc = w - h * cph;
-            *(uint4 *)(kd + (int64_t)(h * kBlockTokens + tt) * g.head_bytes + (cc << 4)) = zero;
-            if (!kBf16) {
-                *(uint4 *)(vd + (int64_t)(h * kBlockTokens + tt) * g.head_bytes + (cc << 4)) = zero;
-            } else {
-                unsigned short *v16 = (unsigned short *)vd;
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    if (by_run) {
+        // heads n - run.first, .. + run.len, ..: 16 chunks of each token, then 8 tokens of each row
+        for (int h = n - run.first; h < g.Hkv; h += run.len) {
+            const int tok = tid >> 4, c = tid & 15;
+            uint4 v = zero;
+            if (tok < run.len) v = *(const uint4 *)(a.v + (run.first + tok) * a.v_stride + (int64_t)h * 256 + (c << 4));
+            __syncthreads();
+            s_v[tok * 17 + c] = v;                       // (the run begins the block: a token's position is its number)
+            __syncthreads();
+            const unsigned short *v16 = (const unsigned short *)s_v;
+            const int d = tid >> 1, half = tid & 1;
+            unsigned e[4];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v16[((int64_t)(h * g.D + cc * 8 + k) << 4) + vperm(tt)] = 0;
+            for (int k = 0; k < 4; ++k) {
+                const int t0 = vperm(8 * half + 2 * k), t1 = vperm(8 * half + 2 * k + 1);
+                e[k] = v16[t0 * 136 + d] | ((unsigned)v16[t1 * 136 + d] << 16);
             }
+            *(uint4 *)(vd + (int64_t)h * 4096 + tid * 16) = make_uint4(e[0], e[1], e[2], e[3]);
+        }
+    }
+    if (t == 0 && run.len < kBlockTokens) {
+        const int rows = kBlockTokens - run.len, cpr = g.row_bytes >> 4;
+        for (int c = tid; c < rows * cpr; c += 256) {
+            const int tt = run.len + c / cpr, w = c % cpr, h = w / cph, cc = w - h * cph;
+            *(uint4 *)(kd + (int64_t)(h * kBlockTokens + tt) * g.head_bytes + (cc << 4)) = zero;
+            if (!kBf16) *(uint4 *)(vd + (int64_t)(h * kBlockTokens + tt) * g.head_bytes + (cc << 4)) = zero;
         }
     }
 }
 
-hipError_t launch_rope_append(const Geom &g, const RopeFreq &f, const RopeAppend &a, const Launch &L)
+hipError_t launch_rope_append(const Geom &g, const RopeAppend &a, const Launch &L)
 {
     if (a.n_tokens == 0) return hipSuccess;
-    if (g.esize == 2) TC_LAUNCH(rope_append_kernel<true>, a.n_tokens, 0, L, f, g, a);
-    else TC_LAUNCH(rope_append_kernel<false>, a.n_tokens, 0, L, f, g, a);
+    if (g.esize == 2) TC_LAUNCH(rope_append_kernel<true>, a.n_tokens, 0, L, g, a);
+    else TC_LAUNCH(rope_append_kernel<false>, a.n_tokens, 0, L, g, a);
     return hipGetLastError();
 }
 
@@ -250,7 +276,12 @@ hipError_t launch_rope_append(const Geom &g, const RopeFreq &f, const RopeAppend
 //
 // One read of the keys: a wave takes one block of one KV head, 16 rows that stand behind one another, and holds 16 bytes of each
 // fourth (or second) row in a lane.  Maximum and minimum are taken on the bits, made to order like integers, in which
-// an infinity or a NaN is an extreme of its sign and so is seen at the end.
+// an infinity or a NaN is an extreme of its sign and so is seen at the end; in that order the complement stands for the negative
+// value, so the lower bounds are upper bounds too from there on.  Between lanes two registers at a time are combined by
+// exchanging rows, after which each lane holds its own two or four bounds and makes bytes of those alone: half the vector
+// work of a reduction in which every lane ends up with all.  Bound: memory.  6168 blocks, 8 heads, two layers, 404 MB read and 25
+// written: 85.5 us = 5.0 TB/s, a large copy's 5.2 (68 us without the writes; loops over several pairs a wave, with the
+// next one's loads ahead, 90 .. 95).
 template <bool kBf16>
 struct Sortable;
 template <>
@@ -268,73 +299,82 @@ struct Sortable<false> {
     __device__ static __forceinline__ float value(vec x, int) { return __int_as_float(flip(x)[0]); }
 };
 
+// Two registers, each to be combined over lanes kApart apart (16 or 32): the first one's result in the lower lanes, the second one's in
+// the others.
+template <int kApart, typename V>
+__device__ __forceinline__ V max_both(V x, V y)
+{
+    const unsigned u = __builtin_bit_cast(unsigned, x), v = __builtin_bit_cast(unsigned, y);
+    unsigned p, q;
+    if (kApart == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(u, v, false, false);
+        p = r[0]; q = r[1];
+    } else {
+        const auto r = __builtin_amdgcn_permlane32_swap(u, v, false, false);
+        p = r[0]; q = r[1];
+    }
+    return __builtin_elementwise_max(__builtin_bit_cast(V, p), __builtin_bit_cast(V, q));
+}
+
 template <bool kBf16, int kLanes>                        // kLanes: 16-byte chunks of a key row, 16 or 32
 __global__ __launch_bounds__(256) void digest_kernel(Geom g, DigestArgs a)
 {
     typedef typename Sortable<kBf16>::vec vec;
-    constexpr int kRowsAt = 64 / kLanes, kLoads = kBlockTokens / kRowsAt, kElems = kBf16 ? 8 : 4;
-    const int lane = threadIdx.x & 63;
+    constexpr int kRowsAt = 64 / kLanes, kLoads = kBlockTokens / kRowsAt, kPer = Sortable<kBf16>::kPerWord;
+    constexpr int kWords = kLanes == 16 ? 2 : 4, kOwn = kWords * kPer;       // bounds a lane ends up with
+    const int lane = threadIdx.x & 63, row = lane / kLanes, c = lane % kLanes;
     const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
     const int i = unit / g.Hkv, h = unit - i * g.Hkv, layer = a.l0 + blockIdx.y;
     if (i >= a.n) return;
     const int32_t entry = a.entries[i];
-    if (entry < 0 || entry_bid(entry) >= g.n_blocks || entry_bid(entry) < a.first_block) return;
-    const int bid = entry_bid(entry), last = kBlockTokens - 1 - entry_pad(entry);       // the last row that holds a key
+    const int bid = entry_bid(entry), last = kBlockTokens - 1 - entry_pad(entry);        // the last row that holds a key
+    if (entry < 0 || bid >= g.n_blocks || bid < a.first_block) return;
     const char *k = g.pool + (int64_t)layer * g.layer_stride + (int64_t)bid * g.block_bytes + (int64_t)h * kBlockTokens * g.head_bytes;
-    const int row = lane / kLanes, c = lane % kLanes;
     union { uint4 u; vec v[4]; } x[kLoads];
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) x[j].u = *(const uint4 *)(k + min(row + j * kRowsAt, last) * g.head_bytes + c * 16);
     vec hi[4], lo[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) hi[q] = lo[q] = Sortable<kBf16>::flip(x[0].v[q]);
+    for (int w = 0; w < 4; ++w) hi[w] = lo[w] = Sortable<kBf16>::flip(x[0].v[w]);
 #pragma unroll
     for (int j = 1; j < kLoads; ++j)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const vec y = Sortable<kBf16>::flip(x[j].v[q]);
-            hi[q] = __builtin_elementwise_max(hi[q], y);
-            lo[q] = __builtin_elementwise_min(lo[q], y);
+        for (int w = 0; w < 4; ++w) {
+            const vec y = Sortable<kBf16>::flip(x[j].v[w]);
+            hi[w] = __builtin_elementwise_max(hi[w], y);
+            lo[w] = __builtin_elementwise_min(lo[w], y);
         }
+    vec own[4];
 #pragma unroll
-    for (int m = kLanes; m < 64; m <<= 1)
+    for (int w = 0; w < 4; ++w) own[w] = max_both<kLanes>(hi[w], ~lo[w]);
+    if (kLanes == 16) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            hi[q] = __builtin_elementwise_max(hi[q], __builtin_bit_cast(vec, __shfl_xor(__builtin_bit_cast(int, hi[q]), m)));
-            lo[q] = __builtin_elementwise_min(lo[q], __builtin_bit_cast(vec, __shfl_xor(__builtin_bit_cast(int, lo[q]), m)));
-        }
-    float up[kElems], dn[kElems];
-    uint32_t size = 0;                                   // of the largest bound, as bits (they order like the sizes)
-#pragma unroll
-    for (int e = 0; e < kElems; ++e) {
-        up[e] = Sortable<kBf16>::value(hi[e / Sortable<kBf16>::kPerWord], e % Sortable<kBf16>::kPerWord);
-        dn[e] = Sortable<kBf16>::value(lo[e / Sortable<kBf16>::kPerWord], e % Sortable<kBf16>::kPerWord);
-        size = max(size, max(__float_as_uint(up[e]) & 0x7fffffffu, __float_as_uint(dn[e]) & 0x7fffffffu));
+        for (int w = 0; w < 2; ++w) own[w] = max_both<32>(own[w], own[w + 2]);
     }
+    const bool is_lo = (lane & kLanes) != 0;
+    const int at = (is_lo ? g.D : 0) + c * (4 * kPer) + (kLanes == 16 ? (lane >> 5) * kOwn : 0);
+    float bound[kOwn];                                   // upper bounds, and lower ones negated
+    uint32_t size = 0;                                   // of the largest, as bits (they order like the sizes)
 #pragma unroll
-    for (int m = 1; m < kLanes; m <<= 1) size = max(size, (uint32_t)__shfl_xor((int)size, m));
+    for (int e = 0; e < kOwn; ++e) {
+        bound[e] = Sortable<kBf16>::value(own[e / kPer], e % kPer);
+        size = max(size, __float_as_uint(bound[e]) & 0x7fffffffu);
+    }
+    size = wave_max(size);
     const bool finite = size < 0x7f800000u;
     const int e = finite ? step_exponent(__uint_as_float(size)) : 127;
     const float by = finite ? step_pow2(-e) : 0.f;
-    // lanes of row group 0 write the upper bounds, those of the last one the lower bounds
-    if (row == 0 || row == kRowsAt - 1) {
-        uint32_t out[kElems / 4];
+    uint32_t bytes = 0;
 #pragma unroll
-        for (int w = 0; w < kElems / 4; ++w) {
-            uint32_t b = 0;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float y = row == 0 ? ceilf(up[4 * w + q] * by) : floorf(dn[4 * w + q] * by);
-                b |= ((uint32_t)(finite ? (int)y : 0) & 0xffu) << (8 * q);
-            }
-            out[w] = b;
-        }
-        const int64_t at = ((int64_t)layer * g.Hkv + h) * g.n_blocks + bid;
-        int8_t *dst = a.digests + at * 2 * g.D + (row == 0 ? 0 : g.D) + c * kElems;
-        if (kBf16) *(uint2 *)dst = make_uint2(out[0], out[kElems / 4 - 1]);
-        else *(uint32_t *)dst = out[0];
-        if (lane == 0) a.digests[a.exps_at + at] = (int8_t)e;
+    for (int q = 0; q < kOwn; ++q) {
+        const float y = ceilf(bound[q] * by);
+        bytes |= ((uint32_t)(finite ? (int)(is_lo ? -y : y) : 0) & 0xffu) << (8 * q);
     }
+    const int64_t to = ((int64_t)layer * g.Hkv + h) * g.n_blocks + bid;
+    int8_t *dst = a.digests + to * 2 * g.D + at;
+    if (kOwn == 4) *(uint32_t *)dst = bytes;
+    else *(uint16_t *)dst = (uint16_t)bytes;
+    if (lane == 0) a.digests[a.exps_at + to] = (int8_t)e;
 }
 
 hipError_t launch_digest(const Geom &g, const DigestArgs &a, int l1, const Launch &L)

@@ -1221,10 +1221,12 @@ tc_status tc_rope_append(tc_ctx *ctx, int32_t layer, const void *q, int64_t q_st
     a.q_stride = q_stride * g.esize; a.k_stride = k_stride * g.esize; a.v_stride = v_stride * g.esize;
     a.q_out = (char *)q_out;
     a.pos = pos; a.slot_map = slot_map; a.n_tokens = n_tokens; a.layer = layer;
-    RopeFreq f{};
     const double two_pi = 6.283185307179586476925286766559;
-    for (int j = 0; j < g.D / 2; ++j) f.rev[j] = std::pow(rope_theta, -2.0 * j / g.D) / two_pi;
-    TC_HIP(ctx, timed_launch(ctx, 1, (hipStream_t)stream, [&](const Launch &ln) { return launch_rope_append(g, f, a, ln); }));
+    for (int j = 0; j < 8; ++j) {
+        a.rev_coarse[j] = std::pow(rope_theta, -16.0 * j / g.D) / two_pi;
+        a.rev_fine[j] = std::pow(rope_theta, -2.0 * j / g.D);
+    }
+    TC_HIP(ctx, timed_launch(ctx, 1, (hipStream_t)stream, [&](const Launch &ln) { return launch_rope_append(g, a, ln); }));
     return TC_OK;
 }
 
