@@ -12,140 +12,158 @@ namespace tc {
 // are spare ones, taken in order, requests in order.  A block is new to its sequence exactly if its position 0 is among the
 // step's tokens, so whoever writes that token's slot writes the table entry, and nobody reads an entry that the step writes.
 //
-// Two prefix sums over the requests, of new tokens and of blocks, run as one of 64 bits (34 for the tokens, 30 for the
-// blocks); then a thread for every token, which finds its request by bisection in LDS.  Everything is a few kilobytes: what
-// counts is the chain of dependent steps, so up to kTablesOneWg tokens one work-group does all of it in one launch.  More tokens
-// are written by many work-groups of a second launch, each of which repeats the sums (the first launch's results may stand
-// where its inputs stood, so the second takes its lengths from those).
-constexpr int kTokenBits = 34;
-
+// Two prefix sums over the requests, of new tokens and of blocks; then a thread for every token, which finds its request by bisection
+// in LDS, four tokens side by side.  Everything is a few kilobytes: a few tokens are a chain of dependent steps, one work-group and
+// one launch; of many the instructions count, 150 a token, so each of several work-groups repeats the sums and writes its part (300
+// requests, 4.7 k tokens: 10 us in one work-group).  Where the results are to stand in place of the inputs that the other
+// work-groups still read, the sums are a launch of their own and the second takes the lengths from its results.
 template <int kThreads, bool kScan, bool kFill>
 __global__ __launch_bounds__(kThreads) void step_tables_kernel(StepTables s)
 {
+    constexpr int kWaves = kThreads / 64;
     extern __shared__ int32_t lds[];                    // [B + 1] first token, [B] tokens held, [B] first spare block
-    __shared__ uint64_t s_wave[kThreads / 64];
-    __shared__ int32_t s_bad;
+    __shared__ uint32_t s_tok[2][kWaves], s_blk[2][kWaves], s_bad[2][kWaves];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, B = s.B;
     int32_t *cu = lds, *held = lds + B + 1, *first = held + B;
-    if (tid == 0) s_bad = 0;
-    __syncthreads();
     // (a fill launch of its own finds the step's end lengths, and the cursor behind the step's blocks)
     const bool refused = !kScan && s.status[0] != 0;
     const int32_t used = kScan ? s.spare_used[0] : s.spare_next[0] - (refused ? 0 : s.status[1]);
-    uint64_t carry = 0;
-    bool bad = used < 0 || used > s.n_spare;
-    for (int b0 = 0; b0 < B; b0 += kThreads) {
+    uint64_t n_new = 0;                                 // of the requests so far; a request counts n_tokens at most, a round of them 2^30
+    uint32_t n_blocks = 0;
+    bool bad = refused || used < 0 || used > s.n_spare;
+    int32_t next_new = 0, next_len = 0;                 // the next round's request, ahead
+    auto look_up = [&](int b) {
+        if (b < B) { next_new = s.new_len[b]; next_len = kScan ? s.seq_len[b] : s.end_len[b]; }
+    };
+    look_up(tid);
+    for (int b0 = 0, round = 0; b0 < B; b0 += kThreads, round ^= 1) {
         const int b = b0 + tid;
-        int32_t len = 0, fresh = 0;
+        const int32_t fresh = b < B ? next_new : 0, len = b < B ? next_len - (kScan || refused ? 0 : fresh) : 0;
+        look_up(b + kThreads);
+        bool mine_bad = false;
         if (b < B) {
-            fresh = s.new_len[b];
-            len = kScan ? s.seq_len[b] : s.end_len[b] - (refused ? 0 : fresh);
-            if (len < 0 || fresh < 0 || (int64_t)len + fresh > (int64_t)s.max_blocks * kBlockTokens || fresh > s.n_tokens) {
-                bad = true;
-                fresh = 0;
-            }
+            mine_bad = len < 0 || fresh < 0 || (int64_t)len + fresh > (int64_t)s.max_blocks * kBlockTokens || fresh > s.n_tokens;
         }
-        const uint32_t blocks = (uint32_t)((len + fresh + 15) >> 4) - (uint32_t)((len + 15) >> 4);
-        const uint64_t mine = bad ? 0 : (uint64_t)fresh | ((uint64_t)blocks << kTokenBits);
-        uint64_t x = mine;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint64_t y = __shfl_up((unsigned long long)x, d);
-            if (lane >= d) x += y;
-        }
-        if (lane == 63) s_wave[w] = x;
+        const uint32_t tok = mine_bad ? 0 : fresh, blk = mine_bad ? 0 : (uint32_t)((len + fresh + 15) >> 4) - (uint32_t)((len + 15) >> 4);
+        const uint32_t upto_tok = wave_prefix(tok), upto_blk = wave_prefix(blk);
+        const bool any_bad = __any(mine_bad);
+        if (lane == 63) { s_tok[round][w] = upto_tok; s_blk[round][w] = upto_blk; s_bad[round][w] = any_bad; }
         __syncthreads();
-        uint64_t before = carry;
-        for (int k = 0; k < w; ++k) before += s_wave[k];
-        for (int k = 0; k < kThreads / 64; ++k) carry += s_wave[k];
+        uint32_t before_tok = 0, before_blk = 0, all_tok = 0, all_blk = 0;
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) {
+            const uint32_t t = s_tok[round][k], c = s_blk[round][k];
+            before_tok += k < w ? t : 0;
+            before_blk += k < w ? c : 0;
+            all_tok += t;
+            all_blk += c;
+            bad |= s_bad[round][k] != 0;
+        }
         if (b < B) {
-            const uint64_t at = before + x - mine;
-            cu[b] = (int32_t)min(at & ((1ull << kTokenBits) - 1), (uint64_t)INT32_MAX);
-            first[b] = (int32_t)(at >> kTokenBits);
+            cu[b] = (int32_t)min(n_new + before_tok + upto_tok - tok, (uint64_t)INT32_MAX);
+            first[b] = (int32_t)(n_blocks + before_blk + upto_blk - blk);
             held[b] = len;
         }
-        __syncthreads();
+        n_new += all_tok;
+        n_blocks += all_blk;
     }
-    if (bad) s_bad = 1;
-    __syncthreads();
-    const uint64_t n_new = carry & ((1ull << kTokenBits) - 1);
-    const int32_t n_blocks = (int32_t)(carry >> kTokenBits);
-    int32_t code = refused || s_bad || n_new > (uint64_t)s.n_tokens ? -1 : 0;
-    if (code == 0 && n_blocks > s.n_spare - used) code = -3;
+    int32_t code = bad || n_new > (uint64_t)s.n_tokens ? -1 : 0;
+    if (code == 0 && (int32_t)n_blocks > s.n_spare - used) code = -3;
     const int32_t total = code == 0 ? (int32_t)n_new : 0;
-    if (kScan) {
-        for (int b = tid; b < B; b += kThreads) {
+    if (kScan && blockIdx.x == 0) {
+        for (int b = tid; b < B; b += kThreads) {       // (a thread's own requests)
             s.cu_new[b] = code == 0 ? cu[b] : 0;
             s.end_len[b] = held[b] + (code == 0 ? s.new_len[b] : 0);
         }
         if (tid == 0) {
             s.cu_new[B] = total;
-            s.spare_next[0] = used + (code == 0 ? n_blocks : 0);
+            s.spare_next[0] = used + (code == 0 ? (int32_t)n_blocks : 0);
             s.status[0] = code;
-            s.status[1] = code == -1 ? 0 : n_blocks;
+            s.status[1] = code == -1 ? 0 : (int32_t)n_blocks;
         }
     }
-    if (kFill) {
-        if (tid == 0) cu[B] = total;
-        __syncthreads();
-        for (int n = blockIdx.x * kThreads + tid; n < s.n_tokens; n += gridDim.x * kThreads) {
+    if (!kFill) return;
+    if (tid == 0) cu[B] = INT32_MAX;
+    __syncthreads();
+    constexpr int kSide = 4;
+    int top = 1;
+    while (2 * top < B) top *= 2;
+    for (int n0 = blockIdx.x * (kSide * kThreads) + tid; n0 < s.n_tokens; n0 += gridDim.x * (kSide * kThreads)) {
+        int lo[kSide] = {0, 0, 0, 0};                   // the last request whose first token is not behind the token
+        for (int step = top; step > 0; step >>= 1)
+#pragma unroll
+            for (int k = 0; k < kSide; ++k) {           // (behind the last request stands a number above all)
+                const int mid = min(lo[k] + step, B);
+                lo[k] = cu[mid] <= n0 + k * kThreads ? mid : lo[k];
+            }
+        int32_t pos[kSide], id[kSide];
+        int32_t *entry[kSide];
+        bool fresh[kSide];
+#pragma unroll
+        for (int k = 0; k < kSide; ++k) {
+            const int n = n0 + k * kThreads;
+            pos[k] = id[k] = -1;
+            if (n >= total) continue;
+            const int b = lo[k];
+            pos[k] = held[b] + (n - cu[b]);
+            const int j = pos[k] >> 4, have = (held[b] + 15) >> 4;
+            entry[k] = s.block_table + (int64_t)b * s.max_blocks + j;
+            fresh[k] = j >= have;
+            id[k] = fresh[k] ? s.spare[used + first[b] + (j - have)] : *entry[k];
+        }
+#pragma unroll
+        for (int k = 0; k < kSide; ++k) {
+            const int n = n0 + k * kThreads;
+            if (n >= s.n_tokens) continue;
             int64_t slot = -1;
-            int32_t pos = -1, seq = -1, full = -1;
+            int32_t full = -1;
             if (n < total) {
-                int lo = 0, hi = B;                     // the last request whose first token is not behind n
-                while (hi - lo > 1) {
-                    const int mid = (lo + hi) >> 1;
-                    if (cu[mid] <= n) lo = mid;
-                    else hi = mid;
-                }
-                seq = lo;
-                pos = held[lo] + (n - cu[lo]);
-                const int j = pos >> 4, have = (held[lo] + 15) >> 4;
-                int32_t *entry = s.block_table + (int64_t)lo * s.max_blocks + j;
-                int32_t id;
-                if (j < have) {
-                    id = *entry < 0 ? -1 : entry_bid(*entry);
+                int32_t block;
+                if (fresh[k]) {
+                    block = id[k] < s.first_seq || id[k] >= s.n_blocks ? -1 : id[k];
+                    if ((pos[k] & 15) == 0) *entry[k] = block;
                 } else {
-                    id = s.spare[used + first[lo] + (j - have)];
-                    if (id < s.first_seq || id >= s.n_blocks) id = -1;
-                    if ((pos & 15) == 0) *entry = id;
+                    block = id[k] < 0 ? -1 : entry_bid(id[k]);
                 }
-                if (id >= 0) {
-                    slot = (int64_t)id * kBlockTokens + (pos & 15);
-                    if ((pos & 15) == 15) full = id;
+                if (block >= 0) {
+                    slot = (int64_t)block * kBlockTokens + (pos[k] & 15);
+                    if ((pos[k] & 15) == 15) full = block;
                 }
             }
             s.slot_map[n] = slot;
-            s.token_pos[n] = pos;
-            s.token_seq[n] = seq;
+            s.token_pos[n] = pos[k];
+            s.token_seq[n] = n < total ? lo[k] : -1;
             s.full_block[n] = full;
         }
     }
 }
 
-constexpr int kTablesOneWg = 8192;
+constexpr int kTablesOneWg = 2048;
+
+template <int kThreads, bool kScan, bool kFill>
+static hipError_t launch_tables(const StepTables &s, const Launch &L)
+{
+    static PerDeviceOnce configured;
+    const hipError_t e = configured.run([] {
+        return hipFuncSetAttribute((const void *)step_tables_kernel<kThreads, kScan, kFill>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                   (3 * kStepMaxSeqs + 1) * (int)sizeof(int32_t));
+    });
+    if (e != hipSuccess) return e;
+    const int grid = !kFill || s.n_tokens <= kTablesOneWg ? 1 : (s.n_tokens + 4 * kThreads - 1) / (4 * kThreads);
+    TC_LAUNCH_N((step_tables_kernel<kThreads, kScan, kFill>), grid, kThreads, (3 * (size_t)s.B + 1) * sizeof(int32_t), L, s);
+    return hipGetLastError();
+}
 
 hipError_t launch_step_tables(const StepTables &s, const Launch &L)
 {
-    const size_t lds = (3 * (size_t)s.B + 1) * sizeof(int32_t);
-    static PerDeviceOnce configured;
-    const hipError_t e = configured.run([] {
-        const int most = (3 * kStepMaxSeqs + 1) * (int)sizeof(int32_t);
-        hipError_t e0 = hipFuncSetAttribute((const void *)step_tables_kernel<1024, true, true>, hipFuncAttributeMaxDynamicSharedMemorySize, most);
-        if (e0 == hipSuccess) e0 = hipFuncSetAttribute((const void *)step_tables_kernel<1024, true, false>, hipFuncAttributeMaxDynamicSharedMemorySize, most);
-        if (e0 == hipSuccess) e0 = hipFuncSetAttribute((const void *)step_tables_kernel<1024, false, true>, hipFuncAttributeMaxDynamicSharedMemorySize, most);
-        return e0;
-    });
-    if (e != hipSuccess) return e;
-    if (s.B <= 256 && s.n_tokens <= 1024) {
-        TC_LAUNCH_N((step_tables_kernel<256, true, true>), 1, 256, lds, L, s);
-    } else if (s.n_tokens <= kTablesOneWg) {
-        TC_LAUNCH_N((step_tables_kernel<1024, true, true>), 1, 1024, lds, L, s);
-    } else {
-        TC_LAUNCH_N((step_tables_kernel<1024, true, false>), 1, 1024, lds, L, s);
-        TC_LAUNCH_N((step_tables_kernel<1024, false, true>), (s.n_tokens + 2047) / 2048, 1024, lds, L, s);
+    const bool few = s.B <= 1024;                       // requests: four rounds of 256 at most
+    if (s.n_tokens > kTablesOneWg && (s.end_len == s.seq_len || s.spare_next == s.spare_used)) {
+        const hipError_t e = launch_tables<1024, true, false>(s, L);
+        if (e != hipSuccess) return e;
+        return few ? launch_tables<256, false, true>(s, L) : launch_tables<1024, false, true>(s, L);
     }
-    return hipGetLastError();
+    if (s.n_tokens > kTablesOneWg ? few : s.B <= 256 && s.n_tokens <= 1024) return launch_tables<256, true, true>(s, L);
+    return launch_tables<1024, true, true>(s, L);
 }
 
 // ------------------------------------------------------------------------------------ encode and append
