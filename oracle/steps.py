@@ -88,6 +88,19 @@ def score(q: np.ndarray, bounds: np.ndarray, e: int) -> float:
     return float(best)
 
 
+def scores(q: np.ndarray, bounds: np.ndarray, exps: np.ndarray) -> np.ndarray:
+    """``score`` of many blocks at once: bounds [n][2][D], exps [n] (products of whole numbers, exact in fp64)."""
+    ok = np.isfinite(q).all(axis=1)
+    best = np.full(len(bounds), -np.inf, dtype=np.float32)
+    for row in q[ok]:
+        f = exponent(np.abs(row).max())
+        i = np.rint(row / 2.0 ** f)
+        dot = (bounds[:, 0] @ np.maximum(i, 0) + bounds[:, 1] @ np.minimum(i, 0)).astype(np.float32)
+        with np.errstate(over="ignore", under="ignore", invalid="ignore"):
+            best = np.maximum(best, dot * np.float32(2.0) ** np.float32(f) * np.float32(2.0) ** exps.astype(np.float32))
+    return np.where(exps == 127, np.float32(np.inf), best)
+
+
 def block_list(pos: int, scores, n_sink: int, n_top: int, n_local: int) -> np.ndarray:
     """The list of a token at `pos`; scores(j) for a candidate block j."""
     own = pos // 16

@@ -53,58 +53,70 @@ struct QueryRows {                                       // 16 rows as a wave ho
     float scale[4];                                      // of rows 4 q4 + e, whose products stand in this lane: 2^f, -1 for a row that takes no part
 };
 
-// Row r16 of this lane: `qr` its channels, `counts` whether it is one.  Lane (r16, q4) holds channels 16 q4 .. and 64 + 16 q4 ..
-// (kD = 64: the first only).
+// 16 query rows made ready in LDS by 256 threads, 16 a row: [max(qi, 0) | min(qi, 0)], 16-byte chunk c of row r at c ^ r.  (Made by every
+// wave for itself they were most of a short call's vector work.)
 template <bool kBf16, int kD>
-__device__ __forceinline__ QueryRows<kD> query_rows(const char *qr, bool counts, int q4)
-{
-    constexpr int kSteps = QueryRows<kD>::kSteps;
-    QueryRows<kD> q;
-    float x[kSteps / 2][16];
-    uint32_t size = 0;
-#pragma unroll
-    for (int s = 0; s < kSteps / 2; ++s)
-#pragma unroll
-        for (int c = 0; c < (kBf16 ? 2 : 4); ++c) {
-            const uint4 v = *(const uint4 *)(qr + (64 * s + 16 * q4) * (kBf16 ? 2 : 4) + c * 16);
+struct QueryTile {
+    static constexpr int kChunks = 2 * kD / 16, kOwn = kD / 16;          // channels of a thread
+    int8_t (&rows)[16 * 2 * kD];
+    float (&scale)[16];
+
+    // tid 0 .. 255; `qr`: the channels of row tid / 16, `counts`: whether it is one
+    __device__ __forceinline__ void make(const char *qr, bool counts, int tid) const
+    {
+        const int r = tid >> 4, c = tid & 15;
+        float x[kOwn];
+        if (kBf16) {
+            const uint4 v = *(const uint4 *)(qr + c * 16);
             const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (kBf16) {
-                    x[s][8 * c + 2 * k] = __uint_as_float(u[k] << 16);
-                    x[s][8 * c + 2 * k + 1] = __uint_as_float(u[k] & 0xffff0000u);
-                } else {
-                    x[s][4 * c + k] = __uint_as_float(u[k]);
-                }
+            for (int k = 0; k < kOwn; ++k) x[k] = __uint_as_float(k & 1 ? u[k >> 1] & 0xffff0000u : u[k >> 1] << 16);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kOwn / 4; ++j) {
+                const f32x4 v = *(const f32x4 *)(qr + c * (4 * kOwn) + 16 * j);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[4 * j + k] = v[k];
             }
         }
+        float size = 0.f;                                // (as bits: they order like the sizes, those of infinities and NaN above all)
 #pragma unroll
-    for (int s = 0; s < kSteps / 2; ++s)
+        for (int k = 0; k < kOwn; ++k) size = __uint_as_float(max(__float_as_uint(size), __float_as_uint(x[k]) & 0x7fffffffu));
+        size = reduce16(size, [](float p, float q) { return __uint_as_float(max(__float_as_uint(p), __float_as_uint(q))); });
+        const bool finite = __float_as_uint(size) < 0x7f800000u;
+        const int f = finite ? step_exponent(size) : 0;
+        const float by = step_pow2(-f);
+        if (c == 0) scale[r] = finite && counts ? step_pow2(f) : -1.f;
+        uint32_t plus[kOwn / 4], minus[kOwn / 4];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) size = max(size, __float_as_uint(x[s][k]) & 0x7fffffffu);
-    size = max(size, (uint32_t)__shfl_xor((int)size, 16));
-    size = max(size, (uint32_t)__shfl_xor((int)size, 32));
-    const bool finite = size < 0x7f800000u;
-    const int f = finite ? step_exponent(__uint_as_float(size)) : 0;
-    const float by = step_pow2(-f), two_f = finite && counts ? step_pow2(f) : -1.f;
-#pragma unroll
-    for (int s = 0; s < kSteps / 2; ++s)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            uint32_t plus = 0, minus = 0;
+        for (int j = 0; j < kOwn / 4; ++j) {
+            plus[j] = minus[j] = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int i = finite ? (int)rintf(x[s][4 * k + e] * by) : 0;
-                plus |= (uint32_t)max(i, 0) << (8 * e);
-                minus |= ((uint32_t)min(i, 0) & 0xffu) << (8 * e);
+                const int i = finite ? (int)rintf(x[4 * j + e] * by) : 0;
+                plus[j] |= (uint32_t)max(i, 0) << (8 * e);
+                minus[j] |= ((uint32_t)min(i, 0) & 0xffu) << (8 * e);
             }
-            q.a[s][k] = (int)plus;
-            q.a[kSteps / 2 + s][k] = (int)minus;
         }
+        const int at = c * kOwn, chunk = at >> 4, in = at & 15;
+        int8_t *row = rows + r * (2 * kD);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) q.scale[e] = __shfl(two_f, 4 * q4 + e);
-    return q;
-}
+        for (int j = 0; j < kOwn / 4; ++j) {
+            *(uint32_t *)(row + ((chunk ^ (r % kChunks)) << 4) + in + 4 * j) = plus[j];
+            *(uint32_t *)(row + (((chunk + kChunks / 2) ^ (r % kChunks)) << 4) + in + 4 * j) = minus[j];
+        }
+    }
+    __device__ __forceinline__ QueryRows<kD> operands(int r16, int q4) const
+    {
+        QueryRows<kD> q;
+#pragma unroll
+        for (int s = 0; s < QueryRows<kD>::kSteps; ++s) q.a[s] = *(const i32x4 *)(rows + r16 * (2 * kD) + (((4 * s + q4) ^ (r16 % kChunks)) << 4));
+        const f32x4 y = *(const f32x4 *)(scale + 4 * q4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q.scale[e] = y[e];
+        return q;
+    }
+};
 
 // Whether an entry names a block, and where that block's digest stands among those of the layer and KV head; one that does not reads
 // another's.
@@ -112,14 +124,12 @@ __device__ __forceinline__ bool is_block(const Geom &g, const SelectArgs &a, int
 {
     return entry >= 0 && entry_bid(entry) >= a.first_block && entry_bid(entry) < g.n_blocks;
 }
-__device__ __forceinline__ int64_t digest_at(const Geom &g, const SelectArgs &a, int kvh, int32_t entry)
-{
-    return ((int64_t)a.layer * g.Hkv + kvh) * g.n_blocks + (is_block(g, a, entry) ? entry_bid(entry) : a.first_block);
-}
+__device__ __forceinline__ int32_t digest_row(const Geom &g, const SelectArgs &a, int32_t entry) { return is_block(g, a, entry) ? entry_bid(entry) : a.first_block; }
+__device__ __forceinline__ int64_t digest_rows(const Geom &g, const SelectArgs &a, int kvh) { return ((int64_t)a.layer * g.Hkv + kvh) * g.n_blocks; }
 constexpr int kNoBlock = 128;                            // in the place of an exponent; 127 marks a key that is not finite
 __device__ __forceinline__ int block_exponent(const Geom &g, const SelectArgs &a, int kvh, int32_t entry)
 {
-    const int e = a.digests[a.exps_at + digest_at(g, a, kvh, entry)];
+    const int e = a.digests[a.exps_at + digest_rows(g, a, kvh) + digest_row(g, a, entry)];
     return is_block(g, a, entry) ? e : kNoBlock;
 }
 
@@ -130,13 +140,14 @@ template <int kD>
 struct BoundsTile {
     static constexpr int kChunks = 2 * kD / 16, kBytes = 16 * 2 * kD, kLoads = kBytes / 1024;
     uint32_t lds;                                        // 16-byte aligned address of the tile
-    // entry: of block r16, in every quarter of the wave
-    __device__ __forceinline__ void load(const Geom &g, const SelectArgs &a, int kvh, int32_t entry, int lane) const
+    // `rows`: the layer and KV head's first digest; row_of(r): the number of block r's
+    template <typename F>
+    __device__ __forceinline__ void load(const char *rows, int lane, F row_of) const
     {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int row = i * (64 / kChunks) + lane / kChunks, c = (lane % kChunks) ^ (row % kChunks);
-            load_to_lds_each(lds + i * 1024, (const char *)a.digests + digest_at(g, a, kvh, __shfl(entry, row)) * (2 * kD) + c * 16);
+            const int r = i * (64 / kChunks) + lane / kChunks, c = (lane % kChunks) ^ (r % kChunks);
+            load_to_lds_each(lds + i * 1024, rows + (uint64_t)(uint32_t)row_of(r) * (2 * kD) + c * 16);
         }
     }
     // The operands of block r16, quarter q4.
@@ -150,37 +161,47 @@ struct BoundsTile {
     }
 };
 
-// Products of this lane's four rows with its block, each by its row's power of two.
-template <int kD>
-__device__ __forceinline__ f32x4 row_products(const QueryRows<kD> &q, const i32x4 (&b)[QueryRows<kD>::kSteps])
+// Products of this lane's four rows of each tile with its block, each by its row's power of two (the tiles' chains side by side).
+template <int kD, int kTiles>
+__device__ __forceinline__ void tile_products(f32x4 (&p)[kTiles], const QueryRows<kD> (&q)[kTiles], const i32x4 (&b)[QueryRows<kD>::kSteps])
 {
-    i32x4 acc = {0, 0, 0, 0};
+    i32x4 acc[kTiles];
 #pragma unroll
-    for (int s = 0; s < QueryRows<kD>::kSteps; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(q.a[s], b[s], acc, 0, 0, 0);
-    f32x4 p;
+    for (int t = 0; t < kTiles; ++t) acc[t] = i32x4{0, 0, 0, 0};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) p[e] = q.scale[e] < 0.f ? -INFINITY : (float)acc[e] * q.scale[e];
-    return p;
+    for (int s = 0; s < QueryRows<kD>::kSteps; ++s)
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[t].a[s], b[s], acc[t], 0, 0, 0);
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[t][e] = q[t].scale[e] < 0.f ? -INFINITY : (float)acc[t][e] * q[t].scale[e];
 }
 __device__ __forceinline__ float column_max(f32x4 p)     // over the 16 rows, in every quarter
 {
     return max_of_quarters(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])));
 }
 
-// A block's score as bits that order like it: the largest product m of its rows, by the block's own power of two.
-__device__ __forceinline__ uint32_t score_key(float m, int e)
-{
-    m = e == 127 ? INFINITY : e == kNoBlock ? -INFINITY : m * step_pow2(min(e, 126)) + 0.f;       // (+ 0: the two zeros are equal)
-    const uint32_t u = __float_as_uint(m);
-    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
-}
+// A block's score as bits that order like it: the largest product of its rows, by the block's own power of two.
+struct BlockScale {
+    float by, fixed;                                     // 2^e; what stands for the score where there is no e
+    bool none;
+    __device__ __forceinline__ explicit BlockScale(int e) : by(step_pow2(min(e, 126))), fixed(e == 127 ? INFINITY : -INFINITY), none(e >= 127) {}
+    __device__ __forceinline__ uint32_t key(float m) const
+    {
+        const float x = m * by + 0.f;                    // (+ 0: the two zeros are equal)
+        const uint32_t u = __float_as_uint(none ? fixed : x);
+        return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+    }
+};
 
 // Scores to memory, where one launch for scores and list (below) does not do: a work-group takes a KV head, kTiles * 16 query rows
 // and a range of candidates, a wave 16 blocks at a time.
 //   kTiles = 1   one token (its heads 16 at a time): tokens of many requests, long tables.  More work-groups than tokens
 //                share the digests.
-//   kTiles = 4   64 / G neighbouring tokens: suffixes, whose tokens read the same digests.  Tokens of another request follow with
-//                a pass of their own.
+//   kTiles = 4   4 (16 / G) neighbouring tokens: suffixes, whose tokens read the same digests.  Tokens of another request follow with
+//                a pass of their own.  The products of rows 4 q4 + e of tile t stand in quarter q4 of a wave, so these sixteen
+//                are the heads of 16 / G whole tokens, one after the other, and a token's largest is found in registers.
 constexpr int kScoreBlocks = 512;                        // candidates of a work-group
 
 template <bool kBf16, int kD, int kTiles>
@@ -188,95 +209,102 @@ __global__ __launch_bounds__(256) void score_kernel(Geom g, SelectArgs a)
 {
     typedef BoundsTile<kD> Tile;
     __shared__ __attribute__((aligned(256))) char s_tile[4][2][Tile::kBytes];
-    __shared__ int32_t s_entry[kScoreBlocks], s_exp[kScoreBlocks];
-    __shared__ float s_prod[4][kTiles > 1 ? kTiles * 16 * 17 : 1];
-    __shared__ int2 s_range[kTiles > 1 ? kTiles * 16 : 1];           // the candidates of each token
+    __shared__ int32_t s_row[kScoreBlocks], s_exp[kScoreBlocks];
     const int group = blockIdx.x / (a.score_parts * g.Hkv), rest = blockIdx.x - group * (a.score_parts * g.Hkv);
     const int kvh = rest / a.score_parts, part = rest - kvh * a.score_parts;
     const int n0 = a.n0 + group * a.group_tokens, n1 = min(n0 + a.group_tokens, a.n0 + a.n_tokens);
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, q4 = lane >> 4;
     const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)s_tile[w][0];
     auto tile = [&](int k) { return Tile{ring + (uint32_t)(k & 1) * Tile::kBytes}; };
-    auto rows_at = [&](int row) {                        // of the group's rows, from `row` on
-        const int r = row + r16, tok = kTiles > 1 ? r / g.G : 0, head = kTiles > 1 ? r - tok * g.G : r;
+    __shared__ __attribute__((aligned(16))) int8_t s_q[kTiles][16 * 2 * kD];
+    __shared__ __attribute__((aligned(16))) float s_scale[kTiles][16];
+    auto make_rows = [&](int t, int row0) {              // tile t: the group's rows from row0 on
+        int tok = 0, head = row0 + (tid >> 4);
+        if (kTiles > 1) {
+            const int place = 4 * t + ((tid >> 4) & 3), of_quarter = place / g.G;        // among the quarter's sixteen
+            tok = of_quarter < a.group_tokens / 4 ? (tid >> 6) * (a.group_tokens / 4) + of_quarter : a.group_tokens;
+            head = place - of_quarter * g.G;
+        }
         const bool counts = n0 + tok < n1 && head < g.G;
-        return query_rows<kBf16, kD>(a.q + ((int64_t)min(n0 + tok, n1 - 1) * g.Hq + kvh * g.G + min(head, g.G - 1)) * g.head_bytes, counts, q4);
+        QueryTile<kBf16, kD>{s_q[t], s_scale[t]}.make(a.q + ((int64_t)min(n0 + tok, n1 - 1) * g.Hq + kvh * g.G + min(head, g.G - 1)) * g.head_bytes, counts, tid);
     };
     QueryRows<kD> q[kTiles];
     if (kTiles > 1) {
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) q[t] = rows_at(16 * t);
+        for (int t = 0; t < kTiles; ++t) make_rows(t, 0);
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) q[t] = QueryTile<kBf16, kD>{s_q[t], s_scale[t]}.operands(r16, q4);
     }
+    const char *digests = (const char *)a.digests + digest_rows(g, a, kvh) * (2 * kD);
+    // lane l looks up the group's token l, and what it chooses from
+    int seq_l = -1, pos_l = 0;
+    if (lane < n1 - n0 && !token_place(a.token_seq, a.token_pos, n0 + lane, a.B, a.max_blocks, seq_l, pos_l)) seq_l = -1;
+    const Window win_l(seq_l >= 0 ? pos_l : 0, a.n_sink, a.n_local);
+    const bool scores_l = seq_l >= 0 && win_l.candidates() > a.n_top;
     for (int t0 = n0, t1; t0 < n1; t0 = t1) {
         // tokens t0 .. t1 - 1 of one request, and the candidates that one of them chooses from
-        int seq, pos, j0 = INT32_MAX, j1 = 0;
-        for (t1 = t0; t1 < n1; ++t1) {
-            int s, p;
-            const bool ok = token_place(a.token_seq, a.token_pos, t1, a.B, a.max_blocks, s, p);
-            if (!ok) s = -1;
-            if (t1 == t0) seq = s;
-            else if (s != seq) break;
-            if (!ok) continue;
-            const Window win(p, a.n_sink, a.n_local);
-            if (win.candidates() <= a.n_top) continue;
-            j0 = min(j0, win.first);
-            j1 = max(j1, win.w0);
-            pos = p;
-        }
-        if (j1 <= j0 || j0 + part * kScoreBlocks >= j1) continue;
+        const int seq = __builtin_amdgcn_readlane(seq_l, t0 - n0);
+        const uint64_t other = ~(__ballot(seq_l == seq && lane < n1 - n0) >> (t0 - n0));
+        t1 = t0 + (other ? __builtin_ctzll(other) : 64);
+        const bool mine = scores_l && lane >= t0 - n0 && lane < t1 - n0;
+        int j0 = (int)~wave_max(mine ? ~(uint32_t)win_l.first : 0u);
+        const int j1 = (int)wave_max(mine ? (uint32_t)win_l.w0 : 0u);
+        if (j1 == 0 || j0 + part * kScoreBlocks >= j1) continue;       // (0: none has too many)
         j0 += part * kScoreBlocks;
+        const uint32_t in_run = (uint32_t)(__ballot(mine) >> (q4 * (a.group_tokens / 4)));     // of this quarter's tokens (kTiles > 1: 16 at most)
         const int count = min(kScoreBlocks, j1 - j0), rounds = count > 16 * w ? (count - 16 * w + 63) >> 6 : 0;
         const int32_t *table = a.block_table + (int64_t)seq * a.max_blocks + j0;
         __syncthreads();                                 // (another request's entries were read)
-        if (kTiles > 1 && t0 + tid < t1) {
-            int s, p;
-            const bool ok = token_place(a.token_seq, a.token_pos, t0 + tid, a.B, a.max_blocks, s, p);
-            const Window win(ok ? p : 0, a.n_sink, a.n_local);
-            s_range[t0 + tid - n0] = ok && win.candidates() > a.n_top ? make_int2(win.first, win.w0) : make_int2(0, 0);
-        }
         for (int i = tid; i < kScoreBlocks; i += 256) {
             const int32_t entry = i < count ? table[i] : -1;
-            s_entry[i] = entry;
+            s_row[i] = digest_row(g, a, entry);
             s_exp[i] = i < count ? block_exponent(g, a, kvh, entry) : kNoBlock;
         }
         __syncthreads();
         for (int row0 = 0; row0 < (kTiles > 1 ? 1 : g.G); row0 += 16) {
             if (kTiles == 1) {
-                q[0] = rows_at(row0);
-                asm volatile("" : "+v"(q[0].scale[0]));  // (here, before the counted loads)
+                if (row0 > 0) __syncthreads();
+                make_rows(0, row0);
+                __syncthreads();
+                q[0] = QueryTile<kBf16, kD>{s_q[0], s_scale[0]}.operands(r16, q4);
             }
-            for (int k = 0; k < 2 && k < rounds; ++k) tile(k).load(g, a, kvh, s_entry[64 * k + 16 * w + r16], lane);
+            auto load = [&](int k) { tile(k).load(digests, lane, [&](int r) { return s_row[64 * k + 16 * w + r]; }); };
+            for (int k = 0; k < 2 && k < rounds; ++k) load(k);
             for (int k = 0; k < rounds; ++k) {
                 if (k + 1 < rounds) wait_loads<Tile::kLoads>();
                 else wait_loads<0>();
                 i32x4 b[QueryRows<kD>::kSteps];
                 tile(k).operands(b, r16, q4);
-                if (k + 2 < rounds) tile(k).load(g, a, kvh, s_entry[64 * (k + 2) + 16 * w + r16], lane);
+                if (k + 2 < rounds) load(k + 2);
                 const int i = 64 * k + 16 * w + r16, j = j0 + i;
+                f32x4 p[kTiles];
+                tile_products<kD>(p, q, b);
                 if (kTiles == 1) {
-                    float m = column_max(row_products<kD>(q[0], b));
-                    const Window win(pos, a.n_sink, a.n_local);
-                    uint32_t *at = a.scores + ((int64_t)(t0 - a.n0) * g.Hkv + kvh) * a.score_stride + (j - win.first);
+                    float m = column_max(p[0]);
+                    uint32_t *at = a.scores + ((int64_t)(t0 - a.n0) * g.Hkv + kvh) * a.score_stride + j;
                     if (q4 == 0 && i < count) {
                         if (row0 > 0) m = fmaxf(m, __uint_as_float(*at));      // (of this lane's own earlier rows)
-                        *at = row0 + 16 >= g.G ? score_key(m, s_exp[i]) : __float_as_uint(m);
+                        *at = row0 + 16 >= g.G ? BlockScale(s_exp[i]).key(m) : __float_as_uint(m);
                     }
                 } else {
-                    float *mine = s_prod[w];
+                    const BlockScale block(i < count ? s_exp[i] : kNoBlock);
+                    int head = 0;
+                    uint32_t left = i < count ? in_run : 0;
+                    uint32_t *out = a.scores + ((int64_t)(n0 - a.n0 + q4 * (a.group_tokens / 4)) * g.Hkv + kvh) * a.score_stride + j;
+                    float m = -INFINITY;
 #pragma unroll
                     for (int t = 0; t < kTiles; ++t) {
-                        const f32x4 p = row_products<kD>(q[t], b);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) mine[(16 * t + 4 * q4 + e) * 17 + r16] = p[e];
-                    }
-                    // a token's block: the largest of its G rows
-                    for (int tok = t0 + q4; tok < t1; tok += 4) {
-                        const float *p = mine + (tok - n0) * g.G * 17 + r16;
-                        float m = p[0];
-                        for (int h = 1; h < g.G; ++h) m = fmaxf(m, p[17 * h]);
-                        const int2 own = s_range[tok - n0];
-                        if (i < count && j >= own.x && j < own.y)
-                            a.scores[((int64_t)(tok - a.n0) * g.Hkv + kvh) * a.score_stride + (j - own.x)] = score_key(m, s_exp[i]);
+                        for (int e = 0; e < 4; ++e) {
+                            m = fmaxf(m, p[t][e]);
+                            if (++head < g.G) continue;  // (the same for the whole wave)
+                            head = 0;
+                            if (left & 1) *out = block.key(m);
+                            left >>= 1;
+                            out += a.score_stride * g.Hkv;
+                            m = -INFINITY;
+                        }
                     }
                 }
             }
@@ -298,16 +326,135 @@ __device__ __forceinline__ void write_fixed(const SelectArgs &a, const Window &w
 }
 
 // The n_top best of a token's candidates and, behind ties, the lower ones; written in ascending order between the first
-// blocks and the last.  A work-group per (token, KV head).  The n_top-th largest score is found by bins over the range that
-// still holds it: a histogram of 1024 equal bins between its ends, the bin that the count falls into, and again inside that
-// (at most four rounds; scores that are spread out take two).  A thread holds an odd number of neighbouring candidates, so that
-// one prefix sum over the threads places them and LDS banks do not collide.
-constexpr int kSelectBins = 1024, kSelectLds = 16384;    // candidates kept in LDS; more are read again from the scores
+// blocks and the last.  The n_top-th largest score is found by bins over the range that still holds it: a histogram of 1024 equal
+// bins between its ends, the bin that the count falls into, and again inside that (at most four rounds; scores that are spread
+// out take two).  A thread holds kPer neighbouring candidates, so that one prefix sum over the threads places them.
+constexpr int kSelectBins = 1024;
 
-template <bool kLds>
+template <int kThreads>
+struct PickShared {
+    __attribute__((aligned(16))) uint32_t bins[kSelectBins], lo[kThreads / 64], hi[kThreads / 64], wave[kThreads / 64], found[3];
+};
+
+// The sum of the waves' values before wave w.
+template <int kWaves>
+__device__ __forceinline__ uint32_t before_wave(const uint32_t (&wave)[kWaves], int w)
+{
+    uint32_t sum = 0;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) sum += k < w ? wave[k] : 0;
+    return sum;
+}
+
+// key: of candidates c0 .. c0 + kPer - 1 (of `cand`, at most 65535); s.bins are zero, in all threads' sight.
+template <int kThreads, int kPer>
+__device__ __forceinline__ void pick(PickShared<kThreads> &s, const uint32_t (&key)[kPer], int c0, int cand, int n_top, int first, int32_t *list, int tid)
+{
+    constexpr int kBins = kSelectBins / kThreads;
+    const int lane = tid & 63, w = tid >> 6;
+    uint32_t lo = 0xffffffffu, hi = 0;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k)
+        if (c0 + k < cand) {
+            lo = min(lo, key[k]);
+            hi = max(hi, key[k]);
+        }
+    hi = wave_max(hi);
+    lo = ~wave_max(~lo);
+    if (lane == 0) { s.lo[w] = lo; s.hi[w] = hi; }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kThreads / 64; ++k) { lo = min(lo, s.lo[k]); hi = max(hi, s.hi[k]); }
+    // keys above `hi` are chosen; `want` of those in [lo, hi] are still to be found
+    uint32_t want = n_top;
+    bool whole = false;
+    while (lo < hi) {
+        const int shift = max(0, 22 - (int)__builtin_clz(hi - lo));     // (hi - lo) >> shift < 1024
+#pragma unroll
+        for (int k = 0; k < kPer; ++k)
+            if (c0 + k < cand && key[k] >= lo && key[k] <= hi) atomicAdd(&s.bins[(key[k] - lo) >> shift], 1u);
+        __syncthreads();
+        // counted from the top: thread t holds bins 1023 - kBins t and the next lower ones
+        uint32_t c[kBins], sum = 0;
+#pragma unroll
+        for (int k = 0; k < kBins; ++k) { c[k] = s.bins[kSelectBins - 1 - kBins * tid - k]; sum += c[k]; }
+        const uint32_t x = wave_prefix(sum);
+        if (lane == 63) s.wave[w] = x;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kBins; ++k) s.bins[kSelectBins - 1 - kBins * tid - k] = 0;
+        uint32_t above = before_wave(s.wave, w) + x - sum;
+#pragma unroll
+        for (int k = 0; k < kBins; ++k) {
+            if (above < want && above + c[k] >= want) { s.found[0] = kSelectBins - 1 - kBins * tid - k; s.found[1] = above; s.found[2] = c[k]; }
+            above += c[k];
+        }
+        __syncthreads();
+        whole = want - s.found[1] == s.found[2];         // all of the bin: its lower end is the threshold
+        want -= s.found[1];
+        lo += s.found[0] << shift;
+        hi = shift == 0 ? lo : min(hi, lo + ((1u << shift) - 1));
+        if (whole) break;
+    }
+    // chosen: keys above the threshold, and the first `want` of those at it
+    uint32_t mine = 0;                                   // (keys at the threshold << 16) + keys above it
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        const bool have = c0 + k < cand;
+        mine += have && (whole ? key[k] >= lo : key[k] > lo) ? 1u : have && !whole && key[k] == lo ? 0x10000u : 0u;
+    }
+    const uint32_t x = wave_prefix(mine);
+    if (lane == 63) s.wave[w] = x;                       // (its last reads were before the loop's last barrier)
+    __syncthreads();
+    const uint32_t before = before_wave(s.wave, w) + x - mine;
+    uint32_t above = before & 0xffffu, ties = before >> 16;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        const bool have = c0 + k < cand, over = have && (whole ? key[k] >= lo : key[k] > lo), tie = have && !whole && key[k] == lo;
+        if (over || (tie && ties < want)) list[first + above + min(ties, want)] = first + c0 + k;
+        above += over;
+        ties += tie;
+    }
+}
+
+// Lists from scores in memory: a work-group a (token, KV head), a thread kSelectPer candidates.
+constexpr int kSelectPer = 8, kSelectFew = 256 * kSelectPer;
+
 __global__ __launch_bounds__(256) void select_kernel(Geom g, SelectArgs a)
 {
-    extern __shared__ uint32_t s_key[];
+    __shared__ PickShared<256> s;
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(4)));
+    const int n = a.n0 + blockIdx.x / g.Hkv, kvh = blockIdx.x % g.Hkv, tid = threadIdx.x;
+    int seq, pos;
+    if (!token_place(a.token_seq, a.token_pos, n, a.B, a.max_blocks, seq, pos)) return;
+    const Window win(pos, a.n_sink, a.n_local);
+    const int cand = win.candidates();
+    int32_t *list = a.lists + ((int64_t)n * g.Hkv + kvh) * (a.n_sink + a.n_top + a.n_local);
+    if (cand > a.n_top && a.n_top > 0) {
+        const uint32_t *scores = a.scores + ((int64_t)(n - a.n0) * g.Hkv + kvh) * a.score_stride + win.first;
+        const int c0 = kSelectPer * tid;
+        uint32_t key[kSelectPer];
+#pragma unroll
+        for (int k = 0; k < kSelectPer; k += 4) {
+            u32x4 v = {0, 0, 0, 0};
+            if (c0 + k + 3 < cand) v = *(const u32x4 *)(scores + c0 + k);
+            else if (c0 + k < cand) {                    // (the row's last few)
+                v[0] = scores[c0 + k];
+                v[1] = c0 + k + 1 < cand ? scores[c0 + k + 1] : 0;
+                v[2] = c0 + k + 2 < cand ? scores[c0 + k + 2] : 0;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) key[k + e] = v[e];
+        }
+        *(uint4 *)&s.bins[4 * tid] = make_uint4(0, 0, 0, 0);             // (seen behind pick's first barrier)
+        pick<256>(s, key, c0, cand, a.n_top, win.first, list, tid);
+    }
+    write_fixed(a, win, list, tid, 256);
+}
+
+// The same for tables of more than kSelectFew entries: the scores stay in memory and are read again in every round.
+__global__ __launch_bounds__(256) void select_long_kernel(Geom g, SelectArgs a)
+{
     __shared__ uint32_t s_bins[kSelectBins];
     __shared__ uint32_t s_wave[8], s_found[3];
     const int n = a.n0 + blockIdx.x / g.Hkv, kvh = blockIdx.x % g.Hkv;
@@ -319,11 +466,10 @@ __global__ __launch_bounds__(256) void select_kernel(Geom g, SelectArgs a)
     int32_t *list = a.lists + ((int64_t)n * g.Hkv + kvh) * n_list;
     write_fixed(a, win, list, tid, 256);
     if (cand <= a.n_top || a.n_top == 0) return;
-    const uint32_t *scores = a.scores + ((int64_t)(n - a.n0) * g.Hkv + kvh) * a.score_stride;
+    const uint32_t *scores = a.scores + ((int64_t)(n - a.n0) * g.Hkv + kvh) * a.score_stride + win.first;
     uint32_t lo = 0xffffffffu, hi = 0;
     for (int i = tid; i < cand; i += 256) {
         const uint32_t k = scores[i];
-        if (kLds) s_key[i] = k;
         lo = min(lo, k);
         hi = max(hi, k);
     }
@@ -336,7 +482,7 @@ __global__ __launch_bounds__(256) void select_kernel(Geom g, SelectArgs a)
     __syncthreads();
     lo = min(min(s_wave[0], s_wave[1]), min(s_wave[2], s_wave[3]));
     hi = max(max(s_wave[4], s_wave[5]), max(s_wave[6], s_wave[7]));
-    const uint32_t *keys = kLds ? s_key : scores;
+    const uint32_t *keys = scores;
     const int per = ((cand + 255) / 256) | 1, c0 = min(tid * per, cand), c1 = min(c0 + per, cand);
     // keys above `hi` are chosen; `want` of those in [lo, hi] are still to be found
     uint32_t want = a.n_top;
@@ -411,30 +557,24 @@ __global__ __launch_bounds__(256) void select_kernel(Geom g, SelectArgs a)
 // pays for itself (and for many tokens, one that reads them once for several).
 constexpr int kFusedBlocks = 2048, kFusedItems = 512;
 
-// The sum of the waves' values before wave w, and of all of them.
-__device__ __forceinline__ uint32_t before_wave(const uint32_t (&s_wave)[16], int w)
-{
-    uint32_t sum = 0;
-#pragma unroll
-    for (int k = 0; k < 16; ++k) sum += k < w ? s_wave[k] : 0;
-    return sum;
-}
-
 template <bool kBf16, int kD>
 __global__ __launch_bounds__(1024) void score_select_kernel(Geom g, SelectArgs a)
 {
     extern __shared__ __attribute__((aligned(256))) char s_ring[];       // two tiles a wave
-    __shared__ __attribute__((aligned(16))) uint32_t s_bins[kSelectBins], s_lo[16], s_hi[16], s_wave[16];
-    __shared__ int32_t s_entry[kFusedBlocks];
+    __shared__ PickShared<1024> s_pick;
+    __shared__ int32_t s_row[kFusedBlocks];
     __shared__ float s_prod[kFusedBlocks];
-    __shared__ uint32_t s_found[3];
     const int n = a.n0 + blockIdx.x / g.Hkv, kvh = blockIdx.x % g.Hkv;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, q4 = lane >> 4;
-    auto rows_at = [&](int row0) {
-        return query_rows<kBf16, kD>(a.q + ((int64_t)n * g.Hq + kvh * g.G + min(row0 + r16, g.G - 1)) * g.head_bytes, row0 + r16 < g.G, q4);
+    __shared__ __attribute__((aligned(16))) int8_t s_q[16 * 2 * kD];
+    __shared__ __attribute__((aligned(16))) float s_scale[16];
+    const QueryTile<kBf16, kD> rows{s_q, s_scale};
+    auto make_rows = [&](int row0) {
+        const int r = row0 + (tid >> 4);
+        if (tid < 256) rows.make(a.q + ((int64_t)n * g.Hq + kvh * g.G + min(r, g.G - 1)) * g.head_bytes, r < g.G, tid);
     };
-    QueryRows<kD> q = rows_at(0);                        // (while the token's place is looked up)
-    s_bins[tid] = 0;
+    make_rows(0);                                        // (while the token's place is looked up)
+    s_pick.bins[tid] = 0;
     int seq, pos;
     if (!token_place(a.token_seq, a.token_pos, n, a.B, a.max_blocks, seq, pos)) return;
     const Window win(pos, a.n_sink, a.n_local);
@@ -450,18 +590,26 @@ __global__ __launch_bounds__(1024) void score_select_kernel(Geom g, SelectArgs a
     typedef BoundsTile<kD> Tile;
     const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)s_ring + w * 2 * Tile::kBytes;
     auto tile = [&](int k) { return Tile{ring + (uint32_t)(k & 1) * Tile::kBytes}; };
+    const char *digests = (const char *)a.digests + digest_rows(g, a, kvh) * (2 * kD);
     const int c0 = 2 * tid;
     int32_t entry[2] = {-1, -1};
     int exponent[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k)
-        if (c0 + k < cand) s_entry[c0 + k] = entry[k] = table[c0 + k];
+        if (c0 + k < cand) s_row[c0 + k] = digest_row(g, a, entry[k] = table[c0 + k]);
     __syncthreads();
     const int rounds = cand > 16 * w ? (cand - 16 * w + 255) >> 8 : 0;
-    auto entry_of = [&](int k) { const int i = 256 * k + 16 * w + r16; return i < cand ? s_entry[i] : -1; };
+    auto load = [&](int k) {
+        tile(k).load(digests, lane, [&](int r) { return s_row[min(256 * k + 16 * w + r, cand - 1)]; });
+    };
     for (int row0 = 0; row0 < g.G; row0 += 16) {
-        if (row0 > 0) q = rows_at(row0);
-        for (int k = 0; k < 2 && k < rounds; ++k) tile(k).load(g, a, kvh, entry_of(k), lane);
+        if (row0 > 0) {
+            __syncthreads();
+            make_rows(row0);
+            __syncthreads();
+        }
+        const QueryRows<kD> q[1] = {rows.operands(r16, q4)};
+        for (int k = 0; k < 2 && k < rounds; ++k) load(k);
         if (row0 == 0) {                                 // (needed last: behind the first bounds)
 #pragma unroll
             for (int k = 0; k < 2; ++k) exponent[k] = block_exponent(g, a, kvh, entry[k]);
@@ -471,8 +619,10 @@ __global__ __launch_bounds__(1024) void score_select_kernel(Geom g, SelectArgs a
             else wait_loads<0>();
             i32x4 b[QueryRows<kD>::kSteps];
             tile(k).operands(b, r16, q4);
-            if (k + 2 < rounds) tile(k).load(g, a, kvh, entry_of(k + 2), lane);
-            float m = column_max(row_products<kD>(q, b));
+            if (k + 2 < rounds) load(k + 2);
+            f32x4 p[1];
+            tile_products<kD>(p, q, b);
+            float m = column_max(p[0]);
             const int i = 256 * k + 16 * w + r16;
             if (q4 == 0 && i < cand) {
                 if (row0 > 0) m = fmaxf(m, s_prod[i]);   // (of this wave's own earlier rows)
@@ -481,66 +631,11 @@ __global__ __launch_bounds__(1024) void score_select_kernel(Geom g, SelectArgs a
         }
     }
     __syncthreads();
-    uint32_t key[2] = {0, 0}, lo = 0xffffffffu, hi = 0;
-    bool have[2];
+    uint32_t key[2] = {0, 0};
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        have[k] = c0 + k < cand;
-        if (have[k]) {
-            key[k] = score_key(s_prod[c0 + k], exponent[k]);
-            lo = min(lo, key[k]);
-            hi = max(hi, key[k]);
-        }
-    }
-    hi = wave_max(hi);
-    lo = ~wave_max(~lo);
-    if (lane == 0) { s_lo[w] = lo; s_hi[w] = hi; }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 16; ++k) { lo = min(lo, s_lo[k]); hi = max(hi, s_hi[k]); }
-
-    // ---- the threshold, as in select_kernel; a thread holds two neighbouring candidates, and a bin
-    uint32_t want = a.n_top;
-    bool whole = false;
-    while (lo < hi) {
-        const int shift = max(0, 22 - (int)__builtin_clz(hi - lo));
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-            if (have[k] && key[k] >= lo && key[k] <= hi) atomicAdd(&s_bins[(key[k] - lo) >> shift], 1u);
-        __syncthreads();
-        const uint32_t c = s_bins[kSelectBins - 1 - tid], x = wave_prefix(c);       // counted from the top
-        if (lane == 63) s_wave[w] = x;
-        __syncthreads();
-        s_bins[tid] = 0;
-        const uint32_t upto = before_wave(s_wave, w) + x;
-        if (upto >= want && upto - c < want) { s_found[0] = kSelectBins - 1 - tid; s_found[1] = upto - c; s_found[2] = c; }
-        __syncthreads();
-        whole = want - s_found[1] == s_found[2];         // all of the bin: its lower end is the threshold
-        want -= s_found[1];
-        lo += s_found[0] << shift;
-        hi = shift == 0 ? lo : min(hi, lo + ((1u << shift) - 1));
-        if (whole) break;
-    }
-    // ---- chosen: keys above the threshold, and the first `want` of those at it
-    bool over[2], tie[2];
-    uint32_t mine = 0;                                   // (keys at the threshold << 16) + keys above it
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        over[k] = have[k] && (whole ? key[k] >= lo : key[k] > lo);
-        tie[k] = have[k] && !whole && key[k] == lo;
-        mine += (over[k] ? 1u : 0u) + (tie[k] ? 0x10000u : 0u);
-    }
-    const uint32_t x = wave_prefix(mine);
-    if (lane == 63) s_wave[w] = x;                       // (its last reads were before the loop's last barrier)
-    __syncthreads();
-    const uint32_t before = before_wave(s_wave, w) + x - mine;
-    uint32_t above = before & 0xffffu, ties = before >> 16;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        if (over[k] || (tie[k] && ties < want)) list[win.first + above + min(ties, want)] = win.first + c0 + k;
-        above += over[k];
-        ties += tie[k];
-    }
+    for (int k = 0; k < 2; ++k)
+        if (c0 + k < cand) key[k] = BlockScale(exponent[k]).key(s_prod[c0 + k]);
+    pick<1024>(s_pick, key, c0, cand, a.n_top, win.first, list, tid);
     write_fixed(a, win, list, tid, 1024);                // (last: a barrier behind a store to memory waits for it)
 }
 
@@ -561,8 +656,8 @@ template <bool kBf16, int kD>
 static hipError_t launch_scores(const Geom &g, SelectArgs a, const Launch &L)
 {
     // several tokens a work-group where requests bring more than one each
-    const bool grouped = a.n_tokens > a.B && g.G <= 32;
-    a.group_tokens = grouped ? 64 / g.G : 1;
+    const bool grouped = a.n_tokens > a.B && g.G <= 16;
+    a.group_tokens = grouped ? 4 * (16 / g.G) : 1;
     a.score_parts = (a.max_blocks + kScoreBlocks - 1) / kScoreBlocks;
     const int64_t grid = (int64_t)((a.n_tokens + a.group_tokens - 1) / a.group_tokens) * g.Hkv * a.score_parts;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
@@ -585,13 +680,8 @@ hipError_t launch_select(const Geom &g, const SelectArgs &a, const Launch &L)
                            : g.D == 64 ? launch_scores<false, 64>(g, a, L) : launch_scores<false, 128>(g, a, L);
         if (e != hipSuccess) return e;
     }
-    static PerDeviceOnce configured;
-    const hipError_t e = configured.run([] {
-        return hipFuncSetAttribute((const void *)select_kernel<true>, hipFuncAttributeMaxDynamicSharedMemorySize, kSelectLds * 4);
-    });
-    if (e != hipSuccess) return e;
-    if (most <= kSelectLds) TC_LAUNCH(select_kernel<true>, (unsigned)items, most * 4, L, g, a);
-    else TC_LAUNCH(select_kernel<false>, (unsigned)items, 0, L, g, a);
+    if (most <= kSelectFew) TC_LAUNCH(select_kernel, (unsigned)items, 0, L, g, a);
+    else TC_LAUNCH(select_long_kernel, (unsigned)items, 0, L, g, a);
     return hipGetLastError();
 }
 
@@ -642,7 +732,7 @@ constexpr float kBaRescale = 8.f;                        // weights grow to 2^8 
 template <int kWaves, bool kSplit>
 __global__ __launch_bounds__(64 * kWaves, 2) void block_attn_bf16_kernel(Geom g, BlockAttnArgs a)
 {
-    extern __shared__ __attribute__((aligned(16))) char lds_raw[];
+    extern __shared__ __attribute__((aligned(256))) char lds[];          // (the XOR addressing of the K rows needs them 256-byte aligned)
     const int chunks = (g.G + 15) >> 4;
     const int item = blockIdx.x / a.n_splits, split = blockIdx.x - item * a.n_splits;
     const int n = item / (g.Hkv * chunks), hc = item - n * (g.Hkv * chunks), kvh = hc / chunks, row0 = (hc - kvh * chunks) * 16;
@@ -660,10 +750,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void block_attn_bf16_kernel(Geom g,
     const int32_t *table = a.block_table + (int64_t)seq * a.max_blocks;
     const char *pool = g.pool + (int64_t)a.layer * g.layer_stride + (int64_t)kvh * kBaBlock;
     const int64_t v_half = g.block_bytes >> 1;
-    // the XOR addressing of the K rows needs them 256-byte aligned
-    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds_raw, slack = (256u - (lds_base & 255u)) & 255u;
-    char *lds = lds_raw + slack;
-    const uint32_t lds_w = lds_base + slack + w * kBaWave;
+    const uint32_t lds_w = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + w * kBaWave;
     typedef const __attribute__((address_space(3))) bf16x8 *lds_frag;
 
     bf16x8 qf[4];
@@ -969,10 +1056,10 @@ static hipError_t launch_attn_bf16_waves(const Geom &g, const BlockAttnArgs &a, 
     static PerDeviceOnce configured;
     const hipError_t e = configured.run([] {
         return hipFuncSetAttribute((const void *)block_attn_bf16_kernel<kWaves, kSplit>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                   kWaves * kBaWave + 256);
+                                   kWaves * kBaWave);
     });
     if (e != hipSuccess) return e;
-    TC_LAUNCH_N((block_attn_bf16_kernel<kWaves, kSplit>), grid, 64 * kWaves, kWaves * kBaWave + 256, L, g, a);      // (+ alignment slack)
+    TC_LAUNCH_N((block_attn_bf16_kernel<kWaves, kSplit>), grid, 64 * kWaves, kWaves * kBaWave, L, g, a);
     return hipGetLastError();
 }
 

@@ -47,7 +47,7 @@ struct SelectArgs {
     const int8_t *digests;
     int64_t exps_at;
     int32_t *lists;
-    uint32_t *scores;                         // [tokens of a round][Hkv][score_stride], ordered like the scores
+    uint32_t *scores;                         // [tokens of a round][Hkv][score_stride], by block, bits ordered like the scores
     int64_t score_stride;
     int32_t n0, n_tokens, layer, B, max_blocks, n_sink, n_top, n_local, first_block;    // tokens n0 .. n0 + n_tokens - 1
     int32_t score_parts, group_tokens;        // scores: work-groups along the candidates, and tokens of one

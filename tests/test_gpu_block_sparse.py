@@ -42,16 +42,15 @@ def _want_lists(pool, q, seq, pos, table, digests, sink, top, local, layer=0):
         if not (0 <= b < len(table) and 0 <= p < 16 * table.shape[1]):
             continue
         for h in range(pool.hkv):
-            memo = {}
-
-            def score(j):
-                e = int(table[b, j])
-                bid = e & ((1 << 27) - 1)
-                if e < 0 or not (pool.first <= bid < pool.n):
-                    return -np.inf
-                if bid not in memo:
-                    memo[bid] = S.score(q64[i, h], bounds[layer, h, bid], int(exps[layer, h, bid]))
-                return memo[bid]
+            e = table[b].astype(np.int64)
+            bid = e & ((1 << 27) - 1)
+            ok = (e >= 0) & (bid >= pool.first) & (bid < pool.n)
+            row = np.full(len(e), -np.inf, dtype=np.float32)
+            some = np.unique(bid[ok])
+            if len(some):
+                at = S.scores(q64[i, h], bounds[layer, h, some].astype(np.float64), exps[layer, h, some])
+                row[ok] = at[np.searchsorted(some, bid[ok])]
+            score = row.__getitem__
             out[i, h] = S.block_list(p, score, sink, top, local)
     return out
 
@@ -148,13 +147,60 @@ def test_lists_of_very_long_sequences(max_blocks):
     pool.close()
 
 
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(28, 4, 128, "bf16"), (8, 8, 128, "bf16"), (32, 2, 128, "bf16"), (20, 1, 128, "bf16"),
+                                            (10, 2, 64, "f32"), (8, 2, 128, "f32")])
+def test_lists_of_suffixes(hq, hkv, d, dtype):
+    """Many tokens of a few requests: those of one request share the digests that are read, and groups of them hold tokens of two
+    or three requests, of requests whose candidates are all listed, padded rows in between and at the end."""
+    lens = [300, 40, 2100, 2500, 17]
+    pool = SH.Pool(hq, hkv, d, dtype, 330, slot_blocks=1)
+    pool.fill(13)
+    table = _table(pool, lens, 160, 4)
+    table[3, 7] = -1
+    table[2, 9] = pool.n
+    digests = _digested(pool, table)
+    seq, pos = [], []
+    for b, n_new in ((0, 3), (1, 5), (2, 250), (3, 150), (0, 70), (4, 2), (2, 130)):
+        seq += [b] * n_new
+        pos += list(range(lens[b] - min(n_new, lens[b]), lens[b])) + [lens[b] - 1] * max(0, n_new - lens[b])
+    for i in (9, 100, 101, 300):
+        seq[i] = -1
+    seq += [-1] * 5
+    pos += [0] * 5
+    q = pool.rows(len(seq), hq, 3)
+    q[20, :, 3] = float("nan")
+    got = _lists(pool, q, seq, pos, table, digests, 1, 13, 2)
+    np.testing.assert_array_equal(got, _want_lists(pool, q, seq, pos, table, digests, 1, 13, 2))
+    # in rounds of few tokens
+    small = torch.full((hkv * 160 * 4 * 77,), 0x22, dtype=torch.uint8, device="cuda")
+    np.testing.assert_array_equal(got, _lists(pool, q, seq, pos, table, digests, 1, 13, 2, workspace=small))
+    pool.close()
+
+
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(7, 1, 128, "bf16"), (34, 1, 128, "bf16"), (20, 1, 64, "f32"), (4, 2, 128, "f32")])
+@pytest.mark.parametrize("max_blocks", [2048, 2049, 2700])
+def test_lists_over_tables_of_some_thousand_blocks(hq, hkv, d, dtype, max_blocks):
+    """One token of each request, tables around the length from which scores and list are launches of their own."""
+    pool = SH.Pool(hq, hkv, d, dtype, 500)
+    pool.fill(8)
+    table = np.random.default_rng(max_blocks).integers(0, 500, size=(3, max_blocks))
+    table[1, 5:60:7] = -1
+    digests = _digested(pool, np.arange(500))
+    pos = [16 * max_blocks - 1, 16 * max_blocks - 9, 16 * 520]
+    q = pool.rows(3, hq, 3)
+    for sink, top, local in ((0, 600, 1), (3, 31, 5)):
+        got = _lists(pool, q, [0, 1, 2], pos, table, digests, sink, top, local)
+        np.testing.assert_array_equal(got, _want_lists(pool, q, [0, 1, 2], pos, table, digests, sink, top, local))
+    pool.close()
+
+
 def test_lists_do_not_depend_on_the_workspace():
     pool = SH.Pool(8, 2, 128, "bf16", 120)
     pool.fill(1)
     table = _table(pool, [900, 1000], 70, 3)
     digests = _digested(pool, table)
-    seq, pos = [0, 1] * 9, [890, 999] * 9
-    q = pool.rows(18, 8, 2)
+    seq, pos = [0, 1] * 150, [890, 999] * 150
+    q = pool.rows(300, 8, 2)
     whole = _lists(pool, q, seq, pos, table, digests, 1, 9, 2)
     for tokens in (1, 5):
         ws = torch.full((2 * 70 * 4 * tokens + 3,), 0x11, dtype=torch.uint8, device="cuda")

@@ -54,6 +54,16 @@ def test_score_bounds_every_key():
     assert S.score(q, b, 127) == np.inf and S.score(np.full((1, 64), np.nan), b, e) == -np.inf
 
 
+def test_scores_of_many_blocks_are_the_scores():
+    rng = np.random.default_rng(6)
+    q = rng.standard_normal((5, 32)) * 3
+    q[2, 4] = np.inf
+    dig = [S.digest(rng.standard_normal((16, 32)) * 10.0 ** x) for x in np.linspace(-30, 30, 9)] + [(np.zeros((2, 32), np.int64), 127)]
+    many = S.scores(q, np.stack([b for b, _ in dig]).astype(np.float64), np.array([e for _, e in dig]))
+    assert many.tolist() == [S.score(q, b, e) for b, e in dig]
+    assert (S.scores(q * np.nan, np.stack([b for b, _ in dig]).astype(np.float64), np.array([0] * 10)) == -np.inf).all()
+
+
 def test_block_list_by_hand():
     score = lambda j: {1: 5.0, 2: 7.0, 3: 7.0, 4: 1.0, 5: 7.0}[j]
     assert S.block_list(7 * 16 + 3, score, 1, 2, 2).tolist() == [0, 2, 3, 6, 7]
