@@ -32,15 +32,23 @@ __device__ __forceinline__ bool token_place(const int32_t *token_seq, const int3
     return seq >= 0 && seq < B && pos >= 0 && (pos >> 4) < max_blocks;
 }
 
-// Over lanes 16 and 32 apart, by exchanging rows of a wave (a shuffle through LDS takes ten times as long).
-__device__ __forceinline__ float max_of_quarters(float x)
+// Over lanes 32 apart, and 16 as well where kApart is 16, by exchanging rows of a wave (a shuffle through LDS takes ten times as
+// long).
+template <int kApart, typename F>
+__device__ __forceinline__ float over_lanes(float x, F op)
 {
-    const unsigned u = __float_as_uint(x);
-    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    const unsigned v = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
-    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+    unsigned u = __float_as_uint(x);
+    if (kApart == 16) {
+        const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        const unsigned p = a[0], q = a[1];
+        u = __float_as_uint(op(__uint_as_float(p), __uint_as_float(q)));
+    }
+    const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const unsigned p = b[0], q = b[1];
+    return op(__uint_as_float(p), __uint_as_float(q));
 }
+template <int kApart> __device__ __forceinline__ float max_over(float x) { return over_lanes<kApart>(x, [](float p, float q) { return fmaxf(p, q); }); }
+template <int kApart> __device__ __forceinline__ float sum_over(float x) { return over_lanes<kApart>(x, [](float p, float q) { return p + q; }); }
 
 // ------------------------------------------------------------------------------------ scores
 // i8 matrix instructions, 16 query rows x 16 blocks x 64: A the query rows as [max(qi, 0) | min(qi, 0)], B the bounds [hi | lo]
@@ -179,7 +187,7 @@ __device__ __forceinline__ void tile_products(f32x4 (&p)[kTiles], const QueryRow
 }
 __device__ __forceinline__ float column_max(f32x4 p)     // over the 16 rows, in every quarter
 {
-    return max_of_quarters(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])));
+    return max_over<16>(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])));
 }
 
 // A block's score as bits that order like it: the largest product of its rows, by the block's own power of two.
@@ -210,8 +218,7 @@ __global__ __launch_bounds__(256) void score_kernel(Geom g, SelectArgs a)
     typedef BoundsTile<kD> Tile;
     __shared__ __attribute__((aligned(256))) char s_tile[4][2][Tile::kBytes];
     __shared__ int32_t s_row[kScoreBlocks], s_exp[kScoreBlocks];
-    const int group = blockIdx.x / (a.score_parts * g.Hkv), rest = blockIdx.x - group * (a.score_parts * g.Hkv);
-    const int kvh = rest / a.score_parts, part = rest - kvh * a.score_parts;
+    const int item = a.parts(blockIdx.x), part = blockIdx.x - item * a.score_parts, group = a.heads(item), kvh = item - group * g.Hkv;
     const int n0 = a.n0 + group * a.group_tokens, n1 = min(n0 + a.group_tokens, a.n0 + a.n_tokens);
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, q4 = lane >> 4;
     const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)s_tile[w][0];
@@ -424,7 +431,7 @@ __global__ __launch_bounds__(256) void select_kernel(Geom g, SelectArgs a)
 {
     __shared__ PickShared<256> s;
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(4)));
-    const int n = a.n0 + blockIdx.x / g.Hkv, kvh = blockIdx.x % g.Hkv, tid = threadIdx.x;
+    const int token = a.heads(blockIdx.x), n = a.n0 + token, kvh = blockIdx.x - token * g.Hkv, tid = threadIdx.x;
     int seq, pos;
     if (!token_place(a.token_seq, a.token_pos, n, a.B, a.max_blocks, seq, pos)) return;
     const Window win(pos, a.n_sink, a.n_local);
@@ -457,7 +464,7 @@ __global__ __launch_bounds__(256) void select_long_kernel(Geom g, SelectArgs a)
 {
     __shared__ uint32_t s_bins[kSelectBins];
     __shared__ uint32_t s_wave[8], s_found[3];
-    const int n = a.n0 + blockIdx.x / g.Hkv, kvh = blockIdx.x % g.Hkv;
+    const int token = a.heads(blockIdx.x), n = a.n0 + token, kvh = blockIdx.x - token * g.Hkv;
     int seq, pos;
     if (!token_place(a.token_seq, a.token_pos, n, a.B, a.max_blocks, seq, pos)) return;
     const Window win(pos, a.n_sink, a.n_local);
@@ -564,7 +571,7 @@ __global__ __launch_bounds__(1024) void score_select_kernel(Geom g, SelectArgs a
     __shared__ PickShared<1024> s_pick;
     __shared__ int32_t s_row[kFusedBlocks];
     __shared__ float s_prod[kFusedBlocks];
-    const int n = a.n0 + blockIdx.x / g.Hkv, kvh = blockIdx.x % g.Hkv;
+    const int token = a.heads(blockIdx.x), n = a.n0 + token, kvh = blockIdx.x - token * g.Hkv;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, q4 = lane >> 4;
     __shared__ __attribute__((aligned(16))) int8_t s_q[16 * 2 * kD];
     __shared__ __attribute__((aligned(16))) float s_scale[16];
@@ -661,14 +668,16 @@ static hipError_t launch_scores(const Geom &g, SelectArgs a, const Launch &L)
     a.score_parts = (a.max_blocks + kScoreBlocks - 1) / kScoreBlocks;
     const int64_t grid = (int64_t)((a.n_tokens + a.group_tokens - 1) / a.group_tokens) * g.Hkv * a.score_parts;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
+    a.parts = FastDiv((uint32_t)a.score_parts);
     if (grouped) TC_LAUNCH((score_kernel<kBf16, kD, 4>), (unsigned)grid, 0, L, g, a);
     else TC_LAUNCH((score_kernel<kBf16, kD, 1>), (unsigned)grid, 0, L, g, a);
     return hipGetLastError();
 }
 
-hipError_t launch_select(const Geom &g, const SelectArgs &a, const Launch &L)
+hipError_t launch_select(const Geom &g, SelectArgs a, const Launch &L)
 {
     if (a.n_tokens == 0) return hipSuccess;
+    a.heads = FastDiv((uint32_t)g.Hkv);
     const int most = a.max_blocks;                       // candidates of any token
     const int64_t items = (int64_t)a.n_tokens * g.Hkv;
     if (items > INT32_MAX) return hipErrorInvalidValue;
@@ -703,6 +712,28 @@ __device__ __forceinline__ void write_bf16x4(char *dst, f32x4 x)
 // running maximum and sum, and are combined through LDS at the end.  No wave waits for another before that.
 struct ListUnit { int32_t j, entry; int valid; };
 
+// A row's partial outputs, maxima and sums of kParts waves, `apart` floats from wave to wave: four columns from d on of each, the maximum
+// and the sum at `ml`.
+template <int kParts>
+__device__ __forceinline__ RowSum fold_rows(const float *part, int apart, int ml, int d)
+{
+    RowSum x{-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
+    float2 of[kParts];
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+        of[k] = *(const float2 *)(part + k * apart + ml);
+        x.M = fmaxf(x.M, of[k].x);
+    }
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+        // (no maximum: no keys - its sums are zeros - or only scores that are NaN, and so are they)
+        const float wgt = of[k].x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(of[k].x - x.M);
+        x.L += wgt * of[k].y;
+        x.acc += wgt * *(const f32x4 *)(part + k * apart + d);
+    }
+    return x;
+}
+
 // Block j of a list: its table entry and how many of its positions the token sees (0: none).
 __device__ __forceinline__ ListUnit list_unit(const Geom &g, const BlockAttnArgs &a, int32_t j, const int32_t *table, int pos)
 {
@@ -733,9 +764,9 @@ template <int kWaves, bool kSplit>
 __global__ __launch_bounds__(64 * kWaves, 2) void block_attn_bf16_kernel(Geom g, BlockAttnArgs a)
 {
     extern __shared__ __attribute__((aligned(256))) char lds[];          // (the XOR addressing of the K rows needs them 256-byte aligned)
-    const int chunks = (g.G + 15) >> 4;
-    const int item = blockIdx.x / a.n_splits, split = blockIdx.x - item * a.n_splits;
-    const int n = item / (g.Hkv * chunks), hc = item - n * (g.Hkv * chunks), kvh = hc / chunks, row0 = (hc - kvh * chunks) * 16;
+    const int chunks = (int)a.chunks.by;
+    const int item = a.splits(blockIdx.x), split = blockIdx.x - item * a.n_splits;
+    const int head = a.chunks(item), n = a.heads(head), kvh = head - n * g.Hkv, row0 = (item - head * chunks) * 16;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, q4 = lane >> 4;
     const int rows = min(16, g.G - row0);
     const int32_t *list = a.lists + ((int64_t)n * g.Hkv + kvh) * a.n_list;
@@ -839,7 +870,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void block_attn_bf16_kernel(Geom g,
                     }
             }
             float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-            const float mxs = max_of_quarters(mx) * a.scale_log2;
+            const float mxs = max_over<16>(mx) * a.scale_log2;
             if (__any(mxs > m_run + kBaRescale)) {       // also taken while m_run is still -inf
                 const float m_new = fmaxf(m_run, mxs);
                 const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
@@ -866,8 +897,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void block_attn_bf16_kernel(Geom g,
     }
 
     // the waves' (output, maximum, sum) rows, combined by 32 threads a row, four columns each
-    float l_row = l_lane + __shfl_xor(l_lane, 16);
-    l_row += __shfl_xor(l_row, 32);
+    const float l_row = sum_over<16>(l_lane);
     if (r16 < rows) {
         float *mine = (float *)(lds + w * kBaWave) + r16 * kBaRow;
 #pragma unroll
@@ -877,18 +907,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void block_attn_bf16_kernel(Geom g,
     __syncthreads();
     const int d = 4 * (tid & 31);
     for (int row = tid >> 5; row < rows; row += 2 * kWaves) {
-        RowSum x{-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-        for (int k = 0; k < kWaves; ++k) x.M = fmaxf(x.M, ((const float *)(lds + k * kBaWave))[row * kBaRow + 128]);
-#pragma unroll
-        for (int k = 0; k < kWaves; ++k) {
-            const float *other = (const float *)(lds + k * kBaWave) + row * kBaRow;
-            const float2 ml = *(const float2 *)(other + 128);
-            // (no maximum: no keys - its sums are zeros - or only scores that are NaN, and so are they)
-            const float wgt = ml.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml.x - x.M);
-            x.L += wgt * ml.y;
-            x.acc += wgt * *(const f32x4 *)(other + d);
-        }
+        const RowSum x = fold_rows<kWaves>((const float *)lds + row * kBaRow, kBaWave / (int)sizeof(float), 128, d);
         const int64_t out_row = (int64_t)n * g.Hq + kvh * g.G + row0 + row;
         if (kSplit) {
             *(f32x4 *)(a.part_o + (out_row * a.n_splits + split) * 128 + d) = x.acc;
@@ -901,15 +920,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void block_attn_bf16_kernel(Geom g,
 
 // fp32, heads of 64 or 128: a unit is one block.  A key row is four channels for each of kD / 4 lanes, so a wave scores
 // 64 / (kD / 4) keys at a time, for up to eight rows, and each of its lane groups keeps a maximum and a sum of its own.
+constexpr int kBaF32Rows = 8;
+
 template <int kD, bool kSplit>
 __global__ __launch_bounds__(256, 2) void block_attn_f32_kernel(Geom g, BlockAttnArgs a)
 {
-    constexpr int kLanes = kD / 4, kGroups = 64 / kLanes, kSteps = kBlockTokens / kGroups, kRows = 8, kParts = 4 * kGroups;
-    __shared__ __attribute__((aligned(16))) float s_o[kParts][kRows][kD];
-    __shared__ float s_ml[kParts][kRows][2];
-    const int chunks = (g.G + kRows - 1) / kRows;
-    const int item = blockIdx.x / a.n_splits, split = blockIdx.x - item * a.n_splits;
-    const int n = item / (g.Hkv * chunks), hc = item - n * (g.Hkv * chunks), kvh = hc / chunks, row0 = (hc - kvh * chunks) * kRows;
+    constexpr int kLanes = kD / 4, kGroups = 64 / kLanes, kSteps = kBlockTokens / kGroups, kRows = kBaF32Rows, kRow = kD + 4, kWaves = 4;
+    __shared__ __attribute__((aligned(16))) float s_part[kWaves * kRows * kRow];         // output, maximum, sum
+    const int chunks = (int)a.chunks.by;
+    const int item = a.splits(blockIdx.x), split = blockIdx.x - item * a.n_splits;
+    const int head = a.chunks(item), n = a.heads(head), kvh = head - n * g.Hkv, row0 = (item - head * chunks) * kRows;
     int seq, pos;
     if (!token_place(a.token_seq, a.token_pos, n, a.B, a.max_blocks, seq, pos)) return;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane % kLanes, grp = lane / kLanes;
@@ -928,9 +948,9 @@ __global__ __launch_bounds__(256, 2) void block_attn_f32_kernel(Geom g, BlockAtt
         m_run[r] = -INFINITY;
         l_run[r] = 0.f;
     }
-    for (int k0 = u0 + w; k0 < u1; k0 += 4 * 64) {
-        const ListUnit mine = list_unit(g, a, k0 + 4 * lane < u1 ? list[k0 + 4 * lane] : -1, table, pos);
-        const int n_mine = min(64, (u1 - k0 + 3) >> 2);
+    for (int k0 = u0 + w; k0 < u1; k0 += kWaves * 64) {
+        const ListUnit mine = list_unit(g, a, k0 + kWaves * lane < u1 ? list[k0 + kWaves * lane] : -1, table, pos);
+        const int n_mine = min(64, (u1 - k0 + kWaves - 1) / kWaves);
         for (int k = 0; k < n_mine; ++k) {
             const int valid = __builtin_amdgcn_readlane(mine.valid, k);
             if (valid <= 0) continue;
@@ -972,18 +992,25 @@ __global__ __launch_bounds__(256, 2) void block_attn_f32_kernel(Geom g, BlockAtt
             }
         }
     }
+    // the lane groups' rows, then the waves'
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
-        *(f32x4 *)&s_o[w * kGroups + grp][r][4 * c] = o[r];
-        if (c == 0) { s_ml[w * kGroups + grp][r][0] = m_run[r]; s_ml[w * kGroups + grp][r][1] = l_run[r]; }
+        if (r >= rows) break;
+        const float M = max_over<kLanes>(m_run[r]);
+        const float wgt = m_run[r] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[r] - M);
+        const float l = sum_over<kLanes>(l_run[r] * wgt);
+        f32x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = sum_over<kLanes>(o[r][e] * wgt);
+        float *mine = s_part + (w * kRows + r) * kRow;
+        if (grp == 0) *(f32x4 *)(mine + 4 * c) = y;
+        if (lane == 0) *(float2 *)(mine + kD) = make_float2(M, l);
     }
     __syncthreads();
     constexpr int kThreadsRow = kD / 4;
-    for (int row = tid / kThreadsRow; row < rows; row += 256 / kThreadsRow) {
+    for (int row = tid / kThreadsRow; row < rows; row += 64 * kWaves / kThreadsRow) {
         const int d = 4 * (tid % kThreadsRow);
-        RowSum x{-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-        for (int k = 0; k < kParts; ++k) x.add(s_ml[k][row][0], s_ml[k][row][1], *(const f32x4 *)&s_o[k][row][d]);
+        const RowSum x = fold_rows<kWaves>(s_part + row * kRow, kRows * kRow, kD, d);
         const int64_t out_row = (int64_t)n * g.Hq + kvh * g.G + row0 + row;
         if (kSplit) {
             *(f32x4 *)(a.part_o + (out_row * a.n_splits + split) * kD + d) = x.acc;
@@ -1028,26 +1055,38 @@ __global__ __launch_bounds__(256) void block_merge_kernel(Geom g, BlockAttnArgs 
 }
 
 // Waves of a work-group and ranges of a list.
+//   bf16: a work-group of eight waves reads a list at what a CU takes from memory, some 80 GB/s, so ranges for work-groups of their own
+//   pay for the launch that combines them (4 us with the gap) only beyond kBaRounds units a wave: 128 blocks for each of 32
+//   items 8.3 + 4.3 us in 4 ranges, 15.2 in one; 53 blocks for each of 4 items 7.4 in one, 5.5 + 4.1 in 7.  Items that fill the chip:
+//   four waves, two work-groups a CU, whose starts and ends overlap (5.2 k items of 64 blocks: 152 us; with eight waves 205).
+//   fp32: bound by its own vector work, 400 instructions a block of four rows, so a unit a wave up to two work-groups a CU (24 blocks
+//   for each of 20 items 5.7 + 3.0 us; in one range of eight waves 9.8).
 constexpr int kBaRounds = 6;
 
 struct BaShape { int waves, splits; };
 static BaShape block_attn_shape(int Hq, int Hkv, int esize, int n_tokens, int n_list)
 {
-    const int G = Hq / Hkv, rows = esize == 2 ? 16 : 8;
-    const int64_t items = (int64_t)n_tokens * Hkv * ((G + rows - 1) / rows);
+    const int G = Hq / Hkv, rows = esize == 2 ? 16 : kBaF32Rows;
+    const int64_t items = std::max<int64_t>((int64_t)n_tokens * Hkv * ((G + rows - 1) / rows), 1);
     const int units = esize == 2 ? (n_list + 1) / 2 : n_list;
-    if (esize != 2) {
-        const int64_t want = items > 0 ? 512 / items : 1;
-        return BaShape{4, (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, (units + 3) / 4), 32))};
-    }
+    auto ranges = [&](int64_t most, int64_t at_least) {  // up to `most` work-groups, none with fewer units
+        return (int)std::max<int64_t>(1, std::min<int64_t>({most / items, (units + at_least - 1) / at_least, 32}));
+    };
+    if (esize != 2) return BaShape{4, ranges(512, 4)};
     if (items > 256 || units <= 4) return BaShape{4, 1};
-    if (units <= 8 * kBaRounds || items > 128) return BaShape{8, 1};
-    return BaShape{8, (int)std::min<int64_t>(std::min<int64_t>((units + 15) / 16, 256 / items), 32)};
+    return BaShape{8, units <= 8 * kBaRounds || items > 128 ? 1 : ranges(256, 16)};
 }
 
 int block_attn_splits(int Hq, int Hkv, int esize, int n_tokens, int n_list)
 {
     return block_attn_shape(Hq, Hkv, esize, n_tokens, n_list).splits;
+}
+
+template <int kD, bool kSplit>
+static hipError_t launch_attn_f32(const Geom &g, const BlockAttnArgs &a, unsigned grid, const Launch &L)
+{
+    TC_LAUNCH((block_attn_f32_kernel<kD, kSplit>), grid, 0, L, g, a);
+    return hipGetLastError();
 }
 
 template <int kWaves, bool kSplit>
@@ -1063,25 +1102,23 @@ static hipError_t launch_attn_bf16_waves(const Geom &g, const BlockAttnArgs &a, 
     return hipGetLastError();
 }
 
-hipError_t launch_block_attn(const Geom &g, const BlockAttnArgs &a, const Launch &L)
+hipError_t launch_block_attn(const Geom &g, BlockAttnArgs a, const Launch &L)
 {
     if (a.n_tokens == 0) return hipSuccess;
-    const int rows = g.esize == 2 ? 16 : 8, chunks = (g.G + rows - 1) / rows;
+    const int rows = g.esize == 2 ? 16 : kBaF32Rows, chunks = (g.G + rows - 1) / rows;
     const int64_t grid = (int64_t)a.n_tokens * g.Hkv * chunks * a.n_splits;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
+    a.splits = FastDiv((uint32_t)a.n_splits);
+    a.chunks = FastDiv((uint32_t)chunks);
+    a.heads = FastDiv((uint32_t)g.Hkv);
     const bool split = a.n_splits > 1;
-    if (g.esize == 2) {
-        const int waves = block_attn_shape(g.Hq, g.Hkv, g.esize, a.n_tokens, a.n_list).waves;
-        return split ? launch_attn_bf16_waves<8, true>(g, a, (unsigned)grid, L)
-             : waves == 8 ? launch_attn_bf16_waves<8, false>(g, a, (unsigned)grid, L) : launch_attn_bf16_waves<4, false>(g, a, (unsigned)grid, L);
-    } else if (g.D == 64) {
-        if (split) TC_LAUNCH((block_attn_f32_kernel<64, true>), (unsigned)grid, 0, L, g, a);
-        else TC_LAUNCH((block_attn_f32_kernel<64, false>), (unsigned)grid, 0, L, g, a);
-    } else {
-        if (split) TC_LAUNCH((block_attn_f32_kernel<128, true>), (unsigned)grid, 0, L, g, a);
-        else TC_LAUNCH((block_attn_f32_kernel<128, false>), (unsigned)grid, 0, L, g, a);
-    }
-    return hipGetLastError();
+    const int waves = block_attn_shape(g.Hq, g.Hkv, g.esize, a.n_tokens, a.n_list).waves;
+    const unsigned n = (unsigned)grid;
+    if (g.esize == 2)
+        return split ? launch_attn_bf16_waves<8, true>(g, a, n, L)
+             : waves == 8 ? launch_attn_bf16_waves<8, false>(g, a, n, L) : launch_attn_bf16_waves<4, false>(g, a, n, L);
+    if (g.D == 64) return split ? launch_attn_f32<64, true>(g, a, n, L) : launch_attn_f32<64, false>(g, a, n, L);
+    return split ? launch_attn_f32<128, true>(g, a, n, L) : launch_attn_f32<128, false>(g, a, n, L);
 }
 
 hipError_t launch_block_merge(const Geom &g, const BlockAttnArgs &a, const Launch &L)

@@ -11,6 +11,19 @@ constexpr int kStepMaxSeqs = 8192;            // requests of a step: three integ
 constexpr int kStepMaxTokens = 1 << 20;       // tokens of a step: their sum over the requests stays below 2^34
 constexpr int kRopeMaxAxes = 4;
 
+// Division of 0 <= n < 2^31 by a number fixed at the launch: a multiplication and a shift (scalar ones, where n is the same for a
+// wave; a division proper is a hundred cycles at the start of every short kernel).
+struct FastDiv {
+    uint32_t by, mul, shift;
+    FastDiv() = default;
+    explicit FastDiv(uint32_t d) : by(d), mul(0), shift(0)
+    {
+        while ((1ull << shift) < d) ++shift;
+        mul = (uint32_t)(((1ull << 32) * ((1ull << shift) - d)) / d + 1);
+    }
+    __device__ __forceinline__ int operator()(int n) const { return (int)((__umulhi(mul, (uint32_t)n) + (uint32_t)n) >> shift); }
+};
+
 struct StepTables {
     const int32_t *seq_len, *new_len;
     int32_t *block_table;
@@ -39,6 +52,7 @@ struct DigestArgs {
     int8_t *digests;                          // bounds [L][Hkv][n_blocks][2][D], then exponents [L][Hkv][n_blocks]
     int64_t exps_at;
     int32_t n, l0, first_block;               // first_block: the lowest id whose keys this pool keeps in blocks
+    FastDiv heads;                            // KV heads
 };
 
 struct SelectArgs {
@@ -51,6 +65,7 @@ struct SelectArgs {
     int64_t score_stride;
     int32_t n0, n_tokens, layer, B, max_blocks, n_sink, n_top, n_local, first_block;    // tokens n0 .. n0 + n_tokens - 1
     int32_t score_parts, group_tokens;        // scores: work-groups along the candidates, and tokens of one
+    FastDiv heads, parts;                     // KV heads, score_parts
 };
 
 struct BlockAttnArgs {
@@ -60,6 +75,7 @@ struct BlockAttnArgs {
     float *part_o, *part_ml;                  // [n_tokens][Hq][n_splits] rows, where the lists are split
     float scale_log2;
     int32_t n_tokens, layer, B, max_blocks, n_list, n_splits, first_block;
+    FastDiv splits, chunks, heads;            // n_splits, work-groups along a group's rows, KV heads
 };
 
 // Over a wave's 64 lanes by DPP (a shuffle through LDS takes five times as long): inclusive prefix sums, and the largest.
@@ -133,9 +149,9 @@ int block_attn_splits(int Hq, int Hkv, int esize, int n_tokens, int n_list);
 
 hipError_t launch_step_tables(const StepTables &s, const Launch &L);
 hipError_t launch_rope_append(const Geom &g, const RopeAppend &a, const Launch &L);
-hipError_t launch_digest(const Geom &g, const DigestArgs &a, int l1, const Launch &L);
-hipError_t launch_select(const Geom &g, const SelectArgs &a, const Launch &L);
-hipError_t launch_block_attn(const Geom &g, const BlockAttnArgs &a, const Launch &L);
+hipError_t launch_digest(const Geom &g, DigestArgs a, int l1, const Launch &L);
+hipError_t launch_select(const Geom &g, SelectArgs a, const Launch &L);
+hipError_t launch_block_attn(const Geom &g, BlockAttnArgs a, const Launch &L);
 hipError_t launch_block_merge(const Geom &g, const BlockAttnArgs &a, const Launch &L);
 
 }  // namespace tc

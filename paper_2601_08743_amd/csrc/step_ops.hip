@@ -200,7 +200,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(Geom g, RopeAppend a)
     const int64_t blk = slot >> 4;
     if (slot < 0 || blk < g.first_seq || blk >= g.n_blocks) return;     // a padded row, or no block of a sequence
     const int t = (int)(slot & 15);
-    const int half_d = g.D >> 1, cph = g.head_bytes >> 4, half_c = cph >> 1;
+    const int half_d = g.D >> 1, cph = g.head_bytes >> 4, half_c = cph >> 1, half_log = __builtin_ctz(half_c);   // (chunks of a head: 16 or 32)
     if (tid < half_d) {
         int axis = 0;
         while (tid >= a.section_end[axis]) ++axis;
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(Geom g, RopeAppend a)
     const int rot_units = (g.Hq + g.Hkv) * half_c, units = rot_units + (by_run ? 0 : g.Hkv * cph);
     for (int u = tid; u < units; u += 256) {
         if (u < rot_units) {
-            const int h = u / half_c, cc = u - h * half_c;
+            const int h = u >> half_log, cc = u & (half_c - 1);
             const bool is_q = h < g.Hq;
             const char *src = (is_q ? a.q + n * a.q_stride + (int64_t)h * g.head_bytes : a.k + n * a.k_stride + (int64_t)(h - g.Hq) * g.head_bytes) + (cc << 4);
             char *dst = (is_q ? a.q_out + ((int64_t)n * g.Hq + h) * g.head_bytes : kd + (int64_t)((h - g.Hq) * kBlockTokens + t) * g.head_bytes) + (cc << 4);
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(Geom g, RopeAppend a)
             *(uint4 *)dst = x;
             *(uint4 *)(dst + (half_c << 4)) = y;
         } else {
-            const int r = u - rot_units, h = r / cph, cc = r - h * cph;
+            const int r = u - rot_units, h = r >> (half_log + 1), cc = r & (cph - 1);
             const uint4 v = *(const uint4 *)(a.v + n * a.v_stride + (int64_t)h * g.head_bytes + (cc << 4));
             if (!kBf16) {
                 *(uint4 *)(vd + (int64_t)(h * kBlockTokens + t) * g.head_bytes + (cc << 4)) = v;
@@ -342,7 +342,7 @@ __global__ __launch_bounds__(256) void digest_kernel(Geom g, DigestArgs a)
     constexpr int kWords = kLanes == 16 ? 2 : 4, kOwn = kWords * kPer;       // bounds a lane ends up with
     const int lane = threadIdx.x & 63, row = lane / kLanes, c = lane % kLanes;
     const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-    const int i = unit / g.Hkv, h = unit - i * g.Hkv, layer = a.l0 + blockIdx.y;
+    const int i = a.heads(unit), h = unit - i * g.Hkv, layer = a.l0 + blockIdx.y;
     if (i >= a.n) return;
     const int32_t entry = a.entries[i];
     const int bid = entry_bid(entry), last = kBlockTokens - 1 - entry_pad(entry);        // the last row that holds a key
@@ -395,10 +395,12 @@ __global__ __launch_bounds__(256) void digest_kernel(Geom g, DigestArgs a)
     if (lane == 0) a.digests[a.exps_at + to] = (int8_t)e;
 }
 
-hipError_t launch_digest(const Geom &g, const DigestArgs &a, int l1, const Launch &L)
+hipError_t launch_digest(const Geom &g, DigestArgs a, int l1, const Launch &L)
 {
     if (a.n == 0 || l1 <= a.l0) return hipSuccess;
     const int64_t units = (int64_t)a.n * g.Hkv;
+    if (units > INT32_MAX - 3) return hipErrorInvalidValue;
+    a.heads = FastDiv((uint32_t)g.Hkv);
     const dim3 grid((unsigned)((units + 3) / 4), l1 - a.l0);
     if (g.esize == 2) TC_LAUNCH((digest_kernel<true, 16>), grid, 0, L, g, a);
     else if (g.D == 64) TC_LAUNCH((digest_kernel<false, 16>), grid, 0, L, g, a);
