@@ -203,17 +203,82 @@ struct BlockScale {
     }
 };
 
-// Scores to memory, where one launch for scores and list (below) does not do: a work-group takes a KV head, kTiles * 16 query rows
-// and a range of candidates, a wave 16 blocks at a time.
-//   kTiles = 1   one token (its heads 16 at a time): tokens of many requests, long tables.  More work-groups than tokens
-//                share the digests.
-//   kTiles = 4   4 (16 / G) neighbouring tokens: suffixes, whose tokens read the same digests.  Tokens of another request follow with
-//                a pass of their own.  The products of rows 4 q4 + e of tile t stand in quarter q4 of a wave, so these sixteen
-//                are the heads of 16 / G whole tokens, one after the other, and a token's largest is found in registers.
-constexpr int kScoreBlocks = 512;                        // candidates of a work-group
+// Scores to memory, where one launch for scores and list (below) does not do: a work-group takes a KV head and a range of candidates,
+// a wave 16 blocks at a time.
+constexpr int kScoreBlocks = 256;                        // candidates of a work-group
 
-template <bool kBf16, int kD, int kTiles>
-__global__ __launch_bounds__(256) void score_kernel(Geom g, SelectArgs a)
+// One token (its heads 16 at a time): tokens of many requests, long tables.
+template <bool kBf16, int kD>
+__global__ __launch_bounds__(256) void score_token_kernel(Geom g, SelectArgs a)
+{
+    typedef BoundsTile<kD> Tile;
+    constexpr int kRounds = kScoreBlocks / 64;
+    __shared__ __attribute__((aligned(256))) char s_tile[4][2][Tile::kBytes];
+    __shared__ __attribute__((aligned(16))) int8_t s_q[16 * 2 * kD];
+    __shared__ __attribute__((aligned(16))) float s_scale[16];
+    __shared__ int32_t s_row[kScoreBlocks];
+    __shared__ float s_prod[kScoreBlocks];
+    const int item = a.parts(blockIdx.x), part = blockIdx.x - item * a.score_parts, token = a.heads(item), kvh = item - token * g.Hkv, n = a.n0 + token;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, q4 = lane >> 4;
+    const QueryTile<kBf16, kD> rows{s_q, s_scale};
+    auto make_rows = [&](int row0) {
+        const int r = row0 + (tid >> 4);
+        rows.make(a.q + ((int64_t)n * g.Hq + kvh * g.G + min(r, g.G - 1)) * g.head_bytes, r < g.G, tid);
+    };
+    make_rows(0);                                        // (while the token's place is looked up)
+    int seq, pos;
+    if (!token_place(a.token_seq, a.token_pos, n, a.B, a.max_blocks, seq, pos)) return;
+    const Window win(pos, a.n_sink, a.n_local);
+    const int j0 = win.first + part * kScoreBlocks;
+    if (win.candidates() <= a.n_top || j0 >= win.w0) return;
+    const int count = min(kScoreBlocks, win.w0 - j0), rounds = count > 16 * w ? (count - 16 * w + 63) >> 6 : 0;
+    const int32_t entry = tid < count ? a.block_table[(int64_t)seq * a.max_blocks + j0 + tid] : -1;
+    s_row[tid] = digest_row(g, a, entry);
+    __syncthreads();
+    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)s_tile[w][0];
+    auto tile = [&](int k) { return Tile{ring + (uint32_t)(k & 1) * Tile::kBytes}; };
+    const char *digests = (const char *)a.digests + digest_rows(g, a, kvh) * (2 * kD);
+    auto load = [&](int k) { tile(k).load(digests, lane, [&](int r) { return s_row[64 * k + 16 * w + r]; }); };
+    float best[kRounds];
+    int exponent = kNoBlock;
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k) best[k] = -INFINITY;
+    for (int row0 = 0; row0 < g.G; row0 += 16) {
+        if (row0 > 0) {
+            __syncthreads();
+            make_rows(row0);
+            __syncthreads();
+        }
+        const QueryRows<kD> q[1] = {rows.operands(r16, q4)};
+        for (int k = 0; k < 2 && k < rounds; ++k) load(k);
+        if (row0 == 0) exponent = block_exponent(g, a, kvh, entry);      // (needed last: behind the first bounds)
+#pragma unroll
+        for (int k = 0; k < kRounds; ++k) {
+            if (k >= rounds) break;
+            if (k + 1 < rounds) wait_loads<Tile::kLoads>();
+            else wait_loads<0>();
+            i32x4 b[QueryRows<kD>::kSteps];
+            tile(k).operands(b, r16, q4);
+            if (k + 2 < rounds) load(k + 2);
+            f32x4 p[1];
+            tile_products<kD>(p, q, b);
+            best[k] = fmaxf(best[k], column_max(p[0]));
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k)
+        if (q4 == 0) s_prod[64 * k + 16 * w + r16] = best[k];
+    __syncthreads();
+    if (tid < count) a.scores[((int64_t)token * g.Hkv + kvh) * a.score_stride + j0 + tid] = BlockScale(exponent).key(s_prod[tid]);
+}
+
+// 4 (16 / G) neighbouring tokens, four tiles of query rows: suffixes, whose tokens read the same digests.  Tokens of another request
+// follow with a pass of their own.  The products of rows 4 q4 + e of tile t stand in quarter q4 of a wave, so these sixteen
+// are the heads of 16 / G whole tokens, one after the other, and a token's largest is found in registers.
+constexpr int kTiles = 4;
+
+template <bool kBf16, int kD>
+__global__ __launch_bounds__(256) void score_group_kernel(Geom g, SelectArgs a)
 {
     typedef BoundsTile<kD> Tile;
     __shared__ __attribute__((aligned(256))) char s_tile[4][2][Tile::kBytes];
@@ -225,24 +290,18 @@ __global__ __launch_bounds__(256) void score_kernel(Geom g, SelectArgs a)
     auto tile = [&](int k) { return Tile{ring + (uint32_t)(k & 1) * Tile::kBytes}; };
     __shared__ __attribute__((aligned(16))) int8_t s_q[kTiles][16 * 2 * kD];
     __shared__ __attribute__((aligned(16))) float s_scale[kTiles][16];
-    auto make_rows = [&](int t, int row0) {              // tile t: the group's rows from row0 on
-        int tok = 0, head = row0 + (tid >> 4);
-        if (kTiles > 1) {
-            const int place = 4 * t + ((tid >> 4) & 3), of_quarter = place / g.G;        // among the quarter's sixteen
-            tok = of_quarter < a.group_tokens / 4 ? (tid >> 6) * (a.group_tokens / 4) + of_quarter : a.group_tokens;
-            head = place - of_quarter * g.G;
-        }
-        const bool counts = n0 + tok < n1 && head < g.G;
-        QueryTile<kBf16, kD>{s_q[t], s_scale[t]}.make(a.q + ((int64_t)min(n0 + tok, n1 - 1) * g.Hq + kvh * g.G + min(head, g.G - 1)) * g.head_bytes, counts, tid);
+    const int of_group = a.group_tokens / 4;             // tokens of a quarter
+    auto make_rows = [&](int t) {
+        const int place = 4 * t + ((tid >> 4) & 3), of_quarter = place / g.G;            // among the quarter's sixteen
+        const int tok = of_quarter < of_group ? (tid >> 6) * of_group + of_quarter : a.group_tokens, head = place - of_quarter * g.G;
+        QueryTile<kBf16, kD>{s_q[t], s_scale[t]}.make(a.q + ((int64_t)min(n0 + tok, n1 - 1) * g.Hq + kvh * g.G + head) * g.head_bytes, n0 + tok < n1, tid);
     };
     QueryRows<kD> q[kTiles];
-    if (kTiles > 1) {
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) make_rows(t, 0);
-        __syncthreads();
+    for (int t = 0; t < kTiles; ++t) make_rows(t);
+    __syncthreads();
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) q[t] = QueryTile<kBf16, kD>{s_q[t], s_scale[t]}.operands(r16, q4);
-    }
+    for (int t = 0; t < kTiles; ++t) q[t] = QueryTile<kBf16, kD>{s_q[t], s_scale[t]}.operands(r16, q4);
     const char *digests = (const char *)a.digests + digest_rows(g, a, kvh) * (2 * kD);
     // lane l looks up the group's token l, and what it chooses from
     int seq_l = -1, pos_l = 0;
@@ -259,60 +318,41 @@ __global__ __launch_bounds__(256) void score_kernel(Geom g, SelectArgs a)
         const int j1 = (int)wave_max(mine ? (uint32_t)win_l.w0 : 0u);
         if (j1 == 0 || j0 + part * kScoreBlocks >= j1) continue;       // (0: none has too many)
         j0 += part * kScoreBlocks;
-        const uint32_t in_run = (uint32_t)(__ballot(mine) >> (q4 * (a.group_tokens / 4)));     // of this quarter's tokens (kTiles > 1: 16 at most)
+        const uint32_t in_run = (uint32_t)(__ballot(mine) >> (q4 * of_group));     // of this quarter's tokens (16 at most)
         const int count = min(kScoreBlocks, j1 - j0), rounds = count > 16 * w ? (count - 16 * w + 63) >> 6 : 0;
         const int32_t *table = a.block_table + (int64_t)seq * a.max_blocks + j0;
         __syncthreads();                                 // (another request's entries were read)
-        for (int i = tid; i < kScoreBlocks; i += 256) {
-            const int32_t entry = i < count ? table[i] : -1;
-            s_row[i] = digest_row(g, a, entry);
-            s_exp[i] = i < count ? block_exponent(g, a, kvh, entry) : kNoBlock;
-        }
+        const int32_t entry = tid < count ? table[tid] : -1;
+        s_row[tid] = digest_row(g, a, entry);
+        s_exp[tid] = block_exponent(g, a, kvh, entry);
         __syncthreads();
-        for (int row0 = 0; row0 < (kTiles > 1 ? 1 : g.G); row0 += 16) {
-            if (kTiles == 1) {
-                if (row0 > 0) __syncthreads();
-                make_rows(0, row0);
-                __syncthreads();
-                q[0] = QueryTile<kBf16, kD>{s_q[0], s_scale[0]}.operands(r16, q4);
-            }
-            auto load = [&](int k) { tile(k).load(digests, lane, [&](int r) { return s_row[64 * k + 16 * w + r]; }); };
-            for (int k = 0; k < 2 && k < rounds; ++k) load(k);
-            for (int k = 0; k < rounds; ++k) {
-                if (k + 1 < rounds) wait_loads<Tile::kLoads>();
-                else wait_loads<0>();
-                i32x4 b[QueryRows<kD>::kSteps];
-                tile(k).operands(b, r16, q4);
-                if (k + 2 < rounds) load(k + 2);
-                const int i = 64 * k + 16 * w + r16, j = j0 + i;
-                f32x4 p[kTiles];
-                tile_products<kD>(p, q, b);
-                if (kTiles == 1) {
-                    float m = column_max(p[0]);
-                    uint32_t *at = a.scores + ((int64_t)(t0 - a.n0) * g.Hkv + kvh) * a.score_stride + j;
-                    if (q4 == 0 && i < count) {
-                        if (row0 > 0) m = fmaxf(m, __uint_as_float(*at));      // (of this lane's own earlier rows)
-                        *at = row0 + 16 >= g.G ? BlockScale(s_exp[i]).key(m) : __float_as_uint(m);
-                    }
-                } else {
-                    const BlockScale block(i < count ? s_exp[i] : kNoBlock);
-                    int head = 0;
-                    uint32_t left = i < count ? in_run : 0;
-                    uint32_t *out = a.scores + ((int64_t)(n0 - a.n0 + q4 * (a.group_tokens / 4)) * g.Hkv + kvh) * a.score_stride + j;
-                    float m = -INFINITY;
+        auto load = [&](int k) { tile(k).load(digests, lane, [&](int r) { return s_row[64 * k + 16 * w + r]; }); };
+        for (int k = 0; k < 2 && k < rounds; ++k) load(k);
+        for (int k = 0; k < rounds; ++k) {
+            if (k + 1 < rounds) wait_loads<Tile::kLoads>();
+            else wait_loads<0>();
+            i32x4 b[QueryRows<kD>::kSteps];
+            tile(k).operands(b, r16, q4);
+            if (k + 2 < rounds) load(k + 2);
+            const int i = 64 * k + 16 * w + r16, j = j0 + i;
+            f32x4 p[kTiles];
+            tile_products<kD>(p, q, b);
+            const BlockScale block(i < count ? s_exp[i] : kNoBlock);
+            int head = 0;
+            uint32_t left = i < count ? in_run : 0;
+            uint32_t *out = a.scores + ((int64_t)(n0 - a.n0 + q4 * of_group) * g.Hkv + kvh) * a.score_stride + j;
+            float m = -INFINITY;
 #pragma unroll
-                    for (int t = 0; t < kTiles; ++t) {
+            for (int t = 0; t < kTiles; ++t) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            m = fmaxf(m, p[t][e]);
-                            if (++head < g.G) continue;  // (the same for the whole wave)
-                            head = 0;
-                            if (left & 1) *out = block.key(m);
-                            left >>= 1;
-                            out += a.score_stride * g.Hkv;
-                            m = -INFINITY;
-                        }
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    m = fmaxf(m, p[t][e]);
+                    if (++head < g.G) continue;  // (the same for the whole wave)
+                    head = 0;
+                    if (left & 1) *out = block.key(m);
+                    left >>= 1;
+                    out += a.score_stride * g.Hkv;
+                    m = -INFINITY;
                 }
             }
         }
@@ -560,9 +600,10 @@ __global__ __launch_bounds__(256) void select_long_kernel(Geom g, SelectArgs a)
 }
 
 // Scores and list in one launch, for few tokens whose tables are not long: a work-group of sixteen waves a (token, KV head), the
-// scores in LDS.  A CU takes its digests at some 100 GB/s, so beyond kFusedBlocks table entries a launch that spreads them over the chip
-// pays for itself (and for many tokens, one that reads them once for several).
-constexpr int kFusedBlocks = 2048, kFusedItems = 512;
+// scores in LDS.  A CU takes its digests at some 80 GB/s, so beyond kFusedBlocks table entries launches that spread them over the chip
+// are as good or better (four tokens of 8 KV heads, 1.7 k entries: 12.4 us so, 12.0 in two), and many tokens of a request should
+// read them once (above kFusedItems).
+constexpr int kFusedBlocks = 1536, kFusedItems = 512;
 
 template <bool kBf16, int kD>
 __global__ __launch_bounds__(1024) void score_select_kernel(Geom g, SelectArgs a)
@@ -669,8 +710,8 @@ static hipError_t launch_scores(const Geom &g, SelectArgs a, const Launch &L)
     const int64_t grid = (int64_t)((a.n_tokens + a.group_tokens - 1) / a.group_tokens) * g.Hkv * a.score_parts;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
     a.parts = FastDiv((uint32_t)a.score_parts);
-    if (grouped) TC_LAUNCH((score_kernel<kBf16, kD, 4>), (unsigned)grid, 0, L, g, a);
-    else TC_LAUNCH((score_kernel<kBf16, kD, 1>), (unsigned)grid, 0, L, g, a);
+    if (grouped) TC_LAUNCH((score_group_kernel<kBf16, kD>), (unsigned)grid, 0, L, g, a);
+    else TC_LAUNCH((score_token_kernel<kBf16, kD>), (unsigned)grid, 0, L, g, a);
     return hipGetLastError();
 }
 
@@ -1029,19 +1070,23 @@ __global__ __launch_bounds__(256) void block_merge_kernel(Geom g, BlockAttnArgs 
     const int64_t row = (int64_t)blockIdx.x * (256 / kThreadsRow) + threadIdx.x / kThreadsRow;
     const int d = 4 * (threadIdx.x % kThreadsRow);
     if (row >= (int64_t)a.n_tokens * g.Hq) return;
-    int seq, pos;
-    if (!token_place(a.token_seq, a.token_pos, (int)(row / g.Hq), a.B, a.max_blocks, seq, pos)) return;
     RowSum x{-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
     constexpr int kBatch = 8;                            // partials requested before the first is used
-    for (int s0 = 0; s0 < a.n_splits; s0 += kBatch) {
-        float2 ml[kBatch];
-        f32x4 po[kBatch];
+    float2 ml[kBatch];
+    f32x4 po[kBatch];
+    auto fetch = [&](int s0) {
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
             const int64_t at = row * a.n_splits + min(s0 + j, a.n_splits - 1);
             ml[j] = *(const float2 *)(a.part_ml + at * 2);
             po[j] = *(const f32x4 *)(a.part_o + at * kD + d);
         }
+    };
+    fetch(0);                                            // (a padded row's are left over from another call, and not used)
+    int seq, pos;
+    if (!token_place(a.token_seq, a.token_pos, (int)(row / g.Hq), a.B, a.max_blocks, seq, pos)) return;
+    for (int s0 = 0; s0 < a.n_splits; s0 += kBatch) {
+        if (s0 > 0) fetch(s0);
 #pragma unroll
         for (int j = 0; j < kBatch; ++j)
             if (s0 + j < a.n_splits) x.add(ml[j].x, ml[j].y, po[j]);

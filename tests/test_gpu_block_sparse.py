@@ -178,7 +178,7 @@ def test_lists_of_suffixes(hq, hkv, d, dtype):
 
 
 @pytest.mark.parametrize("hq,hkv,d,dtype", [(7, 1, 128, "bf16"), (34, 1, 128, "bf16"), (20, 1, 64, "f32"), (4, 2, 128, "f32")])
-@pytest.mark.parametrize("max_blocks", [2048, 2049, 2700])
+@pytest.mark.parametrize("max_blocks", [1536, 1537, 2048, 2049, 2700])
 def test_lists_over_tables_of_some_thousand_blocks(hq, hkv, d, dtype, max_blocks):
     """One token of each request, tables around the length from which scores and list are launches of their own."""
     pool = SH.Pool(hq, hkv, d, dtype, 500)
