@@ -353,7 +353,8 @@ int32_t tc_attn_kernel(const tc_ctx *ctx);
  * over, and nothing outside the arrays and the pool is read or written.  Every call must be made with the context's
  * device current (else TC_ERR_INVALID) and on a stream ordered behind whatever produced its inputs; calls on different streams
  * may overlap if their outputs and workspaces are different.  Tables that sequences read in place (tc_stitch_alias) must stay
- * pinned until the last such call has been enqueued, for replays of a captured graph until those are done.
+ * pinned until the last such call has been enqueued (a later load that takes a slot waits for the streams of these calls, which must
+ * still exist), for replays of a captured graph until those are done.
  * Limits: 8192 requests and 2^20 tokens in a call, max_blocks <= 2^26, fewer than 2^27 pool blocks.
  *
  * Block layout.  In layer l, K of block b is [Hkv][16][D]; V behind it is [Hkv][16][D] in fp32 and [Hkv][D][16] in bf16, there with
@@ -423,8 +424,8 @@ tc_status tc_rope_append(tc_ctx *ctx, int32_t layer, const void *q, int64_t q_st
 size_t tc_digest_bytes(const tc_config *cfg);
 tc_status tc_digest_blocks(tc_ctx *ctx, int32_t l0, int32_t l1, const int32_t *entries, int32_t n, void *digests, void *stream);
 
-/* Bytes of workspace (256-byte aligned, contents need not be initialised and are not kept) for tc_select_blocks and
- * tc_block_attn of up to n_tokens tokens.  tc_select_blocks makes do with less, down to n_kv_heads * max_blocks * 4.
+/* Bytes of workspace (DEVICE, 16-byte aligned; contents need not be initialised and are not kept) for tc_select_blocks and
+ * tc_block_attn of n_tokens tokens or fewer.  tc_select_blocks makes do with less, down to n_kv_heads * max_blocks * 4.
  * 0: an argument out of range. */
 size_t tc_sparse_workspace_bytes(const tc_config *cfg, int32_t n_tokens, int32_t max_blocks, int32_t n_list);
 
@@ -457,7 +458,8 @@ tc_status tc_select_blocks(tc_ctx *ctx, int32_t layer, const void *q, const int3
  *                 layer or an earlier one) or of the caller's own making.  -1, blocks behind the token's own and entries that
  *                 name no block are passed over; a block listed twice is attended to twice.
  *   out           [n_tokens][Hq][D]; rows whose request or position is none are left as they are
- * Errors: TC_ERR_INVALID; TC_ERR_CAPACITY (workspace; none is needed where tc_sparse_workspace_bytes' partials are zero).
+ * The workspace holds partial results where few tokens' long lists are shared out over work-groups.
+ * Errors: TC_ERR_INVALID; TC_ERR_CAPACITY (workspace).
  */
 tc_status tc_block_attn(tc_ctx *ctx, int32_t layer, const void *q, const int32_t *token_seq, const int32_t *token_pos,
                         int32_t n_tokens, const int32_t *block_table, int32_t B, int32_t max_blocks, const int32_t *lists,

@@ -1127,6 +1127,16 @@ int block_attn_splits(int Hq, int Hkv, int esize, int n_tokens, int n_list)
     return block_attn_shape(Hq, Hkv, esize, n_tokens, n_list).splits;
 }
 
+int block_attn_parts(int Hq, int Hkv, int esize, int n_tokens, int n_list)
+{
+    int most = 0;                                        // (beyond 256 tokens no list is in ranges)
+    for (int n = 1; n <= std::min(n_tokens, 256); ++n) {
+        const int splits = block_attn_splits(Hq, Hkv, esize, n, n_list);
+        if (splits > 1) most = std::max(most, n * splits);
+    }
+    return most;
+}
+
 template <int kD, bool kSplit>
 static hipError_t launch_attn_f32(const Geom &g, const BlockAttnArgs &a, unsigned grid, const Launch &L)
 {

@@ -146,6 +146,8 @@ __device__ __forceinline__ void turn_chunk(uint4 &x, uint4 &y, const float2 *w)
 
 // Work-groups that share a token's list: ranges of its units (two blocks in bf16, one in fp32).
 int block_attn_splits(int Hq, int Hkv, int esize, int n_tokens, int n_list);
+// The most (token, range) partials of a query head that up to n_tokens tokens keep, where lists are shared out.
+int block_attn_parts(int Hq, int Hkv, int esize, int n_tokens, int n_list);
 
 hipError_t launch_step_tables(const StepTables &s, const Launch &L);
 hipError_t launch_rope_append(const Geom &g, const RopeAppend &a, const Launch &L);

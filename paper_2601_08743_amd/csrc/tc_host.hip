@@ -85,6 +85,9 @@ struct tc_ctx {
     hipEvent_t raw_ev = nullptr;           // block-format slots: the raw staging area was last used up to here,
     hipStream_t raw_stream = nullptr;      // on this stream
     bool raw_pending = false;
+    static constexpr int kStepStreams = 32;
+    hipStream_t step_readers[kStepStreams] = {};   // block-format slots: streams with token-step calls, which may read any slot,
+    int32_t n_step_readers = 0;                    // since the last load that waited for them (kStepStreams + 1: more than fit)
     Plan plan;
     int32_t *h_stage = nullptr; size_t h_stage_ints = 0;    // pinned
     StageHalves stage;
@@ -527,6 +530,18 @@ tc_status tc_load_async(tc_ctx *ctx, const int32_t *table_ids, int32_t n, int32_
             TC_HIP(ctx, wait_for_reader(ctx, s, stream));   // a stitch may still be reading the previous occupant
             if (s.ready_pending && s.ready_stream != stream)   // earlier copies into this slot on another stream
                 TC_HIP(ctx, hipStreamWaitEvent(stream, s.ready, 0));
+            if (ctx->n_step_readers > 0) {      // token-step calls: everything enqueued so far on the streams they run on
+                if (ctx->n_step_readers > tc_ctx::kStepStreams) TC_HIP(ctx, hipDeviceSynchronize());
+                else
+                    for (int32_t r = 0; r < ctx->n_step_readers; ++r) {
+                        if (ctx->step_readers[r] == stream) continue;
+                        const int32_t ev = record_read(ctx, ctx->step_readers[r]);
+                        if (ev < 0) return fail(ctx, TC_ERR_HIP, "load: hipEventRecord failed");
+                        TC_HIP(ctx, hipStreamWaitEvent(stream, ctx->read_ring[ev], 0));
+                    }
+                // (a later load on another stream comes behind this one: they take turns in the staging area)
+                ctx->n_step_readers = 0;
+            }
             if (s.reader_pending) {     // attention launches read the previous occupant in place: wait for
                                         // everything enqueued so far on the stream they run on
                 if (s.reader_stream != stream) {
@@ -1097,10 +1112,9 @@ static size_t score_bytes_per_token(const tc_config &c, int32_t max_blocks)
     return (size_t)c.n_kv_heads * (size_t)max_blocks * sizeof(uint32_t);
 }
 
-static size_t block_part_bytes(const tc_config &c, int32_t n_tokens, int32_t n_list)
+static size_t block_part_bytes(const tc_config &c, int64_t parts)
 {
-    const int splits = block_attn_splits(c.n_q_heads, c.n_kv_heads, esize_of(c), n_tokens, n_list);
-    return splits <= 1 ? 0 : (size_t)n_tokens * c.n_q_heads * splits * (size_t)(c.head_dim + 2) * sizeof(float);
+    return (size_t)parts * c.n_q_heads * (size_t)(c.head_dim + 2) * sizeof(float);
 }
 
 // What the device-side calls share: limits, the context's own device, and a pool with block ids that leave room for the counts
@@ -1124,12 +1138,15 @@ static tc_status layer_check(tc_ctx *ctx, const char *what, int32_t layer)
     return TC_OK;
 }
 
-// Launches that may read table slots in place (which, only the device knows): a load that evicts a table waits for them.
+// A launch that may read table slots in place (which, only the device knows): the next load that takes a slot waits for it.
 static void slots_read(tc_ctx *ctx, hipStream_t stream)
 {
     if (ctx->cfg.slot_layout != TC_SLOTS_BLOCKS) return;
-    for (Slot &s : ctx->slots)
-        if (s.table >= 0) { s.reader_stream = stream; s.reader_pending = true; }
+    const int32_t n = ctx->n_step_readers;
+    for (int32_t k = 0; k < std::min(n, tc_ctx::kStepStreams); ++k)
+        if (ctx->step_readers[k] == stream) return;
+    if (n < tc_ctx::kStepStreams) ctx->step_readers[n] = stream;
+    ctx->n_step_readers = std::min(n + 1, tc_ctx::kStepStreams + 1);
 }
 
 static bool misaligned(const void *p, size_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
@@ -1147,7 +1164,7 @@ size_t tc_sparse_workspace_bytes(const tc_config *c, int32_t n_tokens, int32_t m
     if (!config_ok(c) || n_tokens < 0 || n_tokens > kStepMaxTokens || max_blocks < 0 || max_blocks > (1 << 26) || n_list < 1) return 0;
     const size_t one = score_bytes_per_token(*c, max_blocks), all = one * (size_t)n_tokens;
     const size_t scores = std::min(all, std::max(one, kScoreRoundBytes));
-    return (std::max({scores, block_part_bytes(*c, n_tokens, n_list), size_t(1)}) + 255) & ~size_t(255);
+    return (std::max({scores, block_part_bytes(*c, block_attn_parts(c->n_q_heads, c->n_kv_heads, esize_of(*c), n_tokens, n_list)), size_t(1)}) + 255) & ~size_t(255);
 }
 
 tc_status tc_table_entries(tc_ctx *ctx, const int32_t *block_table, int64_t n, int32_t *entries)
@@ -1302,17 +1319,19 @@ tc_status tc_block_attn(tc_ctx *ctx, int32_t layer, const void *q, const int32_t
         return fail(ctx, TC_ERR_INVALID, "block attn: null argument");
     if (misaligned(q, 16) || misaligned(out, 16) || misaligned(workspace, 16)) return fail(ctx, TC_ERR_INVALID, "block attn: tensors must be 16-byte aligned");
     hipStream_t stream = (hipStream_t)stream_;
-    const size_t need = block_part_bytes(ctx->cfg, n_tokens, n_list);
+    const Geom &g = ctx->geom;
+    const int splits = block_attn_splits(g.Hq, g.Hkv, g.esize, n_tokens, n_list);
+    const size_t need = splits > 1 ? block_part_bytes(ctx->cfg, (int64_t)n_tokens * splits) : 0;
     if (need > 0 && (!workspace || workspace_bytes < need))
         return fail(ctx, TC_ERR_CAPACITY, "block attn: the workspace holds %zu bytes, the partials take %zu", workspace ? workspace_bytes : 0, need);
     BlockAttnArgs a{};
     a.q = (const char *)q; a.token_seq = token_seq; a.token_pos = token_pos; a.block_table = block_table; a.lists = lists;
     a.out = (char *)out; a.scale_log2 = sm_scale * 1.4426950408889634f;
     a.n_tokens = n_tokens; a.layer = layer; a.B = B; a.max_blocks = max_blocks; a.n_list = n_list;
-    a.n_splits = block_attn_splits(ctx->geom.Hq, ctx->geom.Hkv, ctx->geom.esize, n_tokens, n_list);
+    a.n_splits = splits;
     a.first_block = (int32_t)first_pool_block(ctx->cfg);
     a.part_o = (float *)workspace;
-    if (need > 0) a.part_ml = a.part_o + (size_t)n_tokens * ctx->geom.Hq * a.n_splits * ctx->geom.D;
+    if (need > 0) a.part_ml = a.part_o + (size_t)n_tokens * g.Hq * splits * g.D;
     TC_HIP(ctx, timed_launch(ctx, 2, stream, [&](const Launch &ln) { return launch_block_attn(ctx->geom, a, ln); }));
     if (a.n_splits > 1) TC_HIP(ctx, timed_launch(ctx, 3, stream, [&](const Launch &ln) { return launch_block_merge(ctx->geom, a, ln); }));
     slots_read(ctx, stream);

@@ -307,6 +307,29 @@ def test_attention_in_one_range_and_many(hq, hkv, d, dtype, n_tokens):
     pool.close()
 
 
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(32, 8, 128, "bf16"), (28, 4, 128, "bf16"), (8, 2, 64, "f32")])
+def test_one_workspace_for_any_number_of_tokens(hq, hkv, d, dtype):
+    """A workspace sized for the largest step serves smaller ones, whose lists are shared out further; its bytes behind what was
+    asked for stay as they were."""
+    pool = SH.Pool(hq, hkv, d, dtype, 300)
+    pool.fill(5)
+    table, rng = SH.i32(np.arange(300)[None]), np.random.default_rng(1)
+    need = pool.B.tc_sparse_workspace_bytes(pool.cfg, 40, 300, 200)
+    ws = torch.full((need + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    lists = SH.i32(rng.integers(0, 280, size=(40, hkv, 200)))
+    q = pool.rows(40, hq, 3)
+    whole = None
+    for n in (40, 31, 16, 9, 8, 5, 4, 3, 2, 1):
+        out = torch.empty_like(q[:n])
+        pool.ctx.tc_block_attn(0, q[:n], SH.i32([0] * n), SH.i32([4790] * n), table, lists[:n], out, 0.1, ws[:need])
+        torch.cuda.synchronize()
+        whole = out.float() if whole is None else whole
+        # (another number of ranges: other roundings, each of 2^-8 of |v| < 5.6, or in fp32 of sums of 3200 keys)
+        assert (out.float() - whole[:n]).abs().max() <= (2 * 2.0 ** -8 * 5.6 if dtype == "bf16" else 2 * 3200 * 2.0 ** -24 * 5.6)
+    assert (ws[need:] == 0x5A).all()
+    pool.close()
+
+
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 128), ("f32", 64)])
 def test_attention_with_extreme_values(dtype, d):
     """Scores far apart (one weight takes all), large ones that are equal, a key of minus infinity, a score of plus infinity, keys and

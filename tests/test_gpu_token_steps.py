@@ -179,6 +179,86 @@ def test_one_captured_step_serves_a_growing_batch(alias, shape):
     dw2.close()
 
 
+def test_a_load_that_evicts_a_table_comes_after_the_steps_that_read_it():
+    """Tables read in place by steps on two streams; unpinned, and their slots taken by loads on a third one and a fourth while
+    the steps may still run.  The steps' rows are those of undisturbed steps."""
+    cfg = W.scaled(W.CONFIGS["c2"], n_layers=2, n_tables=16, tables_per_query=(4, 4), capacity=8, batch=2, suffix_len=(5, 40))
+    import harness as H
+    wl = W.make_workload(cfg)
+    wl.queries[:] = [np.array([0, 1, 2, 3], dtype=np.int32), np.array([4, 5, 6, 7], dtype=np.int32)]
+    rows = []
+    for disturb in (False, True):
+        dw = H.DeviceWorkload(wl, seq_blocks=200, capacity=8, slot_layout=1, load_all=False)
+        dw.ctx.tc_pin_tables(list(range(8)))
+        dw.ctx.tc_load_async(list(range(8)), 0, cfg.n_layers, None)
+        max_blocks = max(sum(-(-int(wl.table_len[t]) // 16) for t in q) for q in wl.queries) + 12
+        bt, pl = dw.ctx.tc_stitch_alias(wl.table_ids, wl.cu_tables, wl.suffix_len, max_blocks)
+        for layer in range(cfg.n_layers):
+            dw.attn_layer(layer, bt, pl)
+        held = np.asarray(pl) + wl.suffix_len
+        loops = [Loop(dw, bt[i:i + 1], held[i:i + 1], 40, 8, 1, bt.shape[1], 2) for i in range(2)]
+        for i, l in enumerate(loops):
+            l.fill(i, [40])
+        torch.cuda.synchronize()
+        streams = [torch.cuda.Stream() for _ in range(4)]
+        for l, s in zip(loops, streams):
+            l.step(wl.sm_scale, s)
+        if disturb:
+            dw.ctx.tc_unpin_tables(list(range(8)))
+            for k, t in enumerate(range(8, 16)):
+                dw.ctx.tc_load_async([t], 0, cfg.n_layers, streams[2 + k % 2])
+        torch.cuda.synchronize()
+        rows.append([l.out.clone() for l in loops])
+        dw.close()
+    for a, b in zip(*rows):
+        assert torch.equal(a, b)
+
+
+def test_a_first_call_may_be_captured():
+    """A program whose first token step is the captured one (in an interpreter of its own: kernels are set up once a process)."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import sys
+sys.path[:0] = [%r, %r]
+import numpy as np, torch
+import step_harness as SH
+pool = SH.Pool(28, 4, 128, "bf16", 200)
+pool.fill(1)
+table, digests = SH.i32(np.arange(200)[None]), pool.digests()
+seq, pos, slot = SH.i32([0] * 3), SH.i32([3000, 3001, 3002]), SH.i64([3000, 3001, 3002])
+q, k, v = pool.rows(3, 28, 1), pool.rows(3, 4, 2), pool.rows(3, 4, 3)
+lists, ws, out, qr = SH.i32(np.zeros((3, 4, 90))), pool.workspace(3, 200, 90), torch.empty_like(q), torch.empty_like(q)
+i = lambda n: SH.i32(np.zeros(n))
+tables = (SH.i32([3000]), SH.i32([3]), table, SH.i32([7]), i(1), i(1), i(1), i(2), SH.i64([0] * 3), i(3), i(3), i(3), i(2))
+def step():
+    s = torch.cuda.current_stream()
+    pool.ctx.tc_step_tables(*tables, s)
+    pool.ctx.tc_rope_append(0, q, k, v, pos, 1e4, slot, qr, stream=s)
+    pool.ctx.tc_digest_blocks(0, 1, table, digests, s)
+    pool.ctx.tc_select_blocks(0, qr, seq, pos, table, digests, 1, 80, 9, lists, ws, s)
+    pool.ctx.tc_block_attn(0, qr, seq, pos, table, lists, out, 0.1, ws, s)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    step()
+graph.replay()
+torch.cuda.synchronize()
+got = out.clone()
+out.zero_()
+graph.replay()
+torch.cuda.synchronize()
+assert torch.equal(got, out)
+step()
+torch.cuda.synchronize()
+assert torch.equal(got, out) and torch.isfinite(out).all()
+print("captured first: ok")
+""" % (os.path.dirname(os.path.dirname(os.path.abspath(__file__))), os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=110)
+    assert r.returncode == 0 and "captured first: ok" in r.stdout, r.stdout + r.stderr
+
+
 def test_a_step_that_finds_no_spare_blocks_does_nothing():
     cfg = W.scaled(W.CONFIGS["c2"], n_layers=1, n_tables=8, tables_per_query=(2, 3), capacity=8, batch=3, suffix_len=(5, 40))
     wl, dw, bt, held = _setup(cfg, False, 20)

@@ -81,6 +81,19 @@ def test_block_attn_is_softmax_attention():
     assert (S.block_attn(q.numpy(), k.numpy()[:0], v.numpy()[:0], 0.3)[0] == 0).all()
 
 
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(28, 4, 128, 1), (8, 2, 64, 0), (40, 8, 128, 1), (33, 1, 128, 0)])
+def test_a_workspace_does_for_fewer_tokens_and_shorter_lists(hq, hkv, d, dtype):
+    from paper_2601_08743_amd import binding as B
+    cfg = B.make_config(1, hq, hkv, d, dtype, 4000, 0, 16)
+    size = lambda n, nl: B.tc_sparse_workspace_bytes(cfg, n, 1, nl)
+    for nl in (1, 5, 60, 100, 129, 500, 4000):
+        sizes = [size(n, nl) for n in list(range(1, 140)) + [256, 257, 600, 5000]]
+        assert sizes == sorted(sizes)
+    for n in (1, 3, 17, 200):
+        sizes = [size(n, nl) for nl in range(1, 700, 13)]
+        assert sizes == sorted(sizes)
+
+
 def test_sizes_and_null_contexts_need_no_gpu():
     from paper_2601_08743_amd import binding as B
     cfg = B.make_config(28, 28, 4, 128, B.TC_BF16, 4000, 40, 600)
