@@ -404,8 +404,9 @@ tc_status tc_step_tables(tc_ctx *ctx, const int32_t *seq_len, const int32_t *new
  *   pos         [n_axes][n_tokens], any int32;  n_axes 1 .. 4;  sections HOST [n_axes], D/2 in sum (NULL: one axis)
  *   slot_map    [n_tokens]; a row whose slot is negative, or in no sequence block, is passed over (q_out too)
  *   q_out       [n_tokens][Hq][D] (may be q, where q_stride is Hq * D)
- * Tokens of one block must stand in position order, as tc_step_tables lists them, and no slot twice.  A block whose first slot
- * is written gets zeros behind the last of these tokens, so that no later call finds leftovers there.
+ * Tokens of one block must stand next to one another in position order, none left out between them, as tc_step_tables lists them,
+ * and no slot twice.  A block whose first slot is written gets zeros behind the last of these tokens, so that no later call finds
+ * leftovers there.
  */
 tc_status tc_rope_append(tc_ctx *ctx, int32_t layer, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                          const void *v, int64_t v_stride, const int32_t *pos, int32_t n_axes, const int32_t *sections,

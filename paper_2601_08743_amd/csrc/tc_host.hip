@@ -1234,6 +1234,7 @@ tc_status tc_rope_append(tc_ctx *ctx, int32_t layer, const void *q, int64_t q_st
     if (misaligned(q, 16) || misaligned(k, 16) || misaligned(v, 16) || misaligned(q_out, 16) || misaligned(slot_map, 8) ||
         ((q_stride | k_stride | v_stride) * g.esize & 15))
         return fail(ctx, TC_ERR_INVALID, "append: rows must be 16-byte aligned");
+    if (q_out == q && n_tokens > 1 && q_stride != (int64_t)g.Hq * g.D) return fail(ctx, TC_ERR_INVALID, "append: q_out would overwrite rows of q");
     a.q = (const char *)q; a.k = (const char *)k; a.v = (const char *)v;
     a.q_stride = q_stride * g.esize; a.k_stride = k_stride * g.esize; a.v_stride = v_stride * g.esize;
     a.q_out = (char *)q_out;

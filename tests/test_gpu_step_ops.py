@@ -314,3 +314,17 @@ def test_table_entries(small_pool):
         with pytest.raises(B.TcError) as e:
             c.tc_table_entries(np.array([5, bad]))
         assert e.value.code == B.TC_ERR_INVALID
+
+
+def test_encoded_queries_do_not_overwrite_rows_still_to_be_read(small_pool):
+    from paper_2601_08743_amd import binding as B
+    p = small_pool
+    wide = p.rows(2, 12, 1)                                                         # queries and keys of one projection
+    q, kv, out = wide[:, :8], wide[:, 8:10], wide.view(-1)[:2 * 8 * 64].view(2, 8, 64)
+    before, slot = wide.clone(), SH.i64([16 * p.first, 16 * p.first + 1])
+    with pytest.raises(B.TcError) as e:
+        p.ctx.tc_rope_append(0, q, kv, kv, SH.i32([1, 2]), 1e4, slot, out)
+    assert e.value.code == B.TC_ERR_INVALID
+    torch.cuda.synchronize()
+    assert torch.equal(wide, before)
+    p.ctx.tc_rope_append(0, q[:1], kv[:1], kv[:1], SH.i32([1]), 1e4, slot[:1], out[:1])        # one row is read before it is written
