@@ -52,8 +52,8 @@ template <int kApart> __device__ __forceinline__ float sum_over(float x) { retur
 
 // ------------------------------------------------------------------------------------ scores
 // i8 matrix instructions, 16 query rows x 16 blocks x 64: A the query rows as [max(qi, 0) | min(qi, 0)], B the bounds [hi | lo]
-// of 16 blocks, straight from memory (a block's 2D bytes are whole lines).  Bound: reading the bounds, 1/16 of the cache's
-// bytes in bf16.
+// of 16 blocks (a block's 2D bytes are whole lines).  Bound: reading the bounds, 1/16 of the cache's bytes in bf16, and for a token
+// or a few the chain of round trips to them: place, table entry, bounds.
 template <int kD>
 struct QueryRows {                                       // 16 rows as a wave holds them
     static constexpr int kSteps = 2 * kD / 64;           // matrix instructions along the 2D products
@@ -207,7 +207,7 @@ struct BlockScale {
 // a wave 16 blocks at a time.
 constexpr int kScoreBlocks = 256;                        // candidates of a work-group
 
-// One token (its heads 16 at a time): tokens of many requests, long tables.
+// One token (its heads 16 at a time): tokens of many requests, long tables (four tokens, 8 KV heads, 1.4 to 1.7 k blocks: 5.9 us).
 template <bool kBf16, int kD>
 __global__ __launch_bounds__(256) void score_token_kernel(Geom g, SelectArgs a)
 {
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(256) void score_token_kernel(Geom g, SelectArgs a)
 }
 
 // 4 (16 / G) neighbouring tokens, four tiles of query rows: suffixes, whose tokens read the same digests.  Tokens of another request
-// follow with a pass of their own.  The products of rows 4 q4 + e of tile t stand in quarter q4 of a wave, so these sixteen
+// follow with a pass of their own.  (681 tokens of eight requests, 8 KV heads, 380 to 849 blocks: 28 us.)  The products of rows 4 q4 + e of tile t stand in quarter q4 of a wave, so these sixteen
 // are the heads of 16 / G whole tokens, one after the other, and a token's largest is found in registers.
 constexpr int kTiles = 4;
 
@@ -464,7 +464,8 @@ __device__ __forceinline__ void pick(PickShared<kThreads> &s, const uint32_t (&k
     }
 }
 
-// Lists from scores in memory: a work-group a (token, KV head), a thread kSelectPer candidates.
+// Lists from scores in memory: a work-group a (token, KV head), a thread kSelectPer candidates.  A chain of barriers: 5.6 us for 32
+// work-groups (118 of 1.7 k), 19 for 5.4 k (60 of some 600).
 constexpr int kSelectPer = 8, kSelectFew = 256 * kSelectPer;
 
 __global__ __launch_bounds__(256) void select_kernel(Geom g, SelectArgs a)
@@ -602,7 +603,7 @@ __global__ __launch_bounds__(256) void select_long_kernel(Geom g, SelectArgs a)
 // Scores and list in one launch, for few tokens whose tables are not long: a work-group of sixteen waves a (token, KV head), the
 // scores in LDS.  A CU takes its digests at some 80 GB/s, so beyond kFusedBlocks table entries launches that spread them over the chip
 // are as good or better (four tokens of 8 KV heads, 1.7 k entries: 12.4 us so, 12.0 in two), and many tokens of a request should
-// read them once (above kFusedItems).
+// read them once (above kFusedItems).  One token of 4 KV heads, 288 entries: 6.0 us; 32 tokens of up to 311: 7.4.
 constexpr int kFusedBlocks = 1536, kFusedItems = 512;
 
 template <bool kBf16, int kD>
@@ -795,6 +796,8 @@ __device__ __forceinline__ ListUnit list_unit(const Geom &g, const BlockAttnArgs
 // from there: loaded straight into the operands' registers, where neighbouring lanes are neighbouring rows of 256 bytes, keys take a
 // CU's address path 64 cycles a kilobyte instead of 16.  The next unit's keys are requested as soon as this one's are in
 // registers, and so the values.  (Values straight to registers, 32-byte rows, and twice the waves: slower for every list tried.)
+// Bound: 53 blocks for each of 4 items, 7.5 us, the chain of units; 49 for each of 128, 51 MB, 11.1 us = 4.6 TB/s, what a CU takes from
+// memory; 64 for each of 5.4 k items, 157 us, the L2's 2.8 GB = 18 TB/s, of which a fifth comes from further (all there: 105 us).
 constexpr int kBaRow = 132;                              // padded output row of the exchange (floats), maximum and sum behind it
 constexpr int kBaBlock = 4096;                           // one head's K (or V) in one block
 constexpr int kBaWave = 4 * kBaBlock;                    // K of a unit: rows of 256 bytes, 16-byte chunk c of row r at c ^ r; V: two blocks verbatim
@@ -1062,7 +1065,8 @@ __global__ __launch_bounds__(256, 2) void block_attn_f32_kernel(Geom g, BlockAtt
     }
 }
 
-// Ranges of a list combined: kD / 4 threads a row.
+// Ranges of a list combined: kD / 4 threads a row, all of a row's first partials requested at once (bound: the launch and one round trip;
+// 128 rows of four ranges 3.6 us).
 template <bool kBf16, int kD>
 __global__ __launch_bounds__(256) void block_merge_kernel(Geom g, BlockAttnArgs a)
 {
@@ -1102,10 +1106,10 @@ __global__ __launch_bounds__(256) void block_merge_kernel(Geom g, BlockAttnArgs 
 // Waves of a work-group and ranges of a list.
 //   bf16: a work-group of eight waves reads a list at what a CU takes from memory, some 80 GB/s, so ranges for work-groups of their own
 //   pay for the launch that combines them (4 us with the gap) only beyond kBaRounds units a wave: 128 blocks for each of 32
-//   items 8.3 + 4.3 us in 4 ranges, 15.2 in one; 53 blocks for each of 4 items 7.4 in one, 5.5 + 4.1 in 7.  Items that fill the chip:
-//   four waves, two work-groups a CU, whose starts and ends overlap (5.2 k items of 64 blocks: 152 us; with eight waves 205).
+//   items 8.7 + 3.6 us in 4 ranges, 15.2 in one; 53 blocks for each of 4 items 7.5 in one, 5.5 + 4.1 in 7.  Items that fill the chip:
+//   four waves, two work-groups a CU, whose starts and ends overlap (5.4 k items of 64 blocks: 157 us; with eight waves 205).
 //   fp32: bound by its own vector work, 400 instructions a block of four rows, so a unit a wave up to two work-groups a CU (24 blocks
-//   for each of 20 items 5.7 + 3.0 us; in one range of eight waves 9.8).
+//   for each of 20 items 5.3 + 2.8 us; in one range of eight waves 9.8).
 constexpr int kBaRounds = 6;
 
 struct BaShape { int waves, splits; };
