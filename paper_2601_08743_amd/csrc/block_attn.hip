@@ -204,7 +204,8 @@ struct BlockScale {
 };
 
 // Scores to memory, where one launch for scores and list (below) does not do: a work-group takes a KV head and a range of candidates,
-// a wave 16 blocks at a time.
+// a wave 16 blocks at a time.  Ranges come behind one another in the grid: the last ones are short or empty, and as neighbours
+// each would belong to chiplets of its own (the case of many tokens below: 28 us).
 constexpr int kScoreBlocks = 256;                        // candidates of a work-group
 
 // One token (its heads 16 at a time): tokens of many requests, long tables (four tokens, 8 KV heads, 1.4 to 1.7 k blocks: 5.9 us).
@@ -218,7 +219,7 @@ __global__ __launch_bounds__(256) void score_token_kernel(Geom g, SelectArgs a)
     __shared__ __attribute__((aligned(16))) float s_scale[16];
     __shared__ int32_t s_row[kScoreBlocks];
     __shared__ float s_prod[kScoreBlocks];
-    const int item = a.parts(blockIdx.x), part = blockIdx.x - item * a.score_parts, token = a.heads(item), kvh = item - token * g.Hkv, n = a.n0 + token;
+    const int part = a.parts(blockIdx.x), item = blockIdx.x - part * (int)a.parts.by, token = a.heads(item), kvh = item - token * g.Hkv, n = a.n0 + token;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, q4 = lane >> 4;
     const QueryTile<kBf16, kD> rows{s_q, s_scale};
     auto make_rows = [&](int row0) {
@@ -273,7 +274,7 @@ __global__ __launch_bounds__(256) void score_token_kernel(Geom g, SelectArgs a)
 }
 
 // 4 (16 / G) neighbouring tokens, four tiles of query rows: suffixes, whose tokens read the same digests.  Tokens of another request
-// follow with a pass of their own.  (681 tokens of eight requests, 8 KV heads, 380 to 849 blocks: 28 us.)  The products of rows 4 q4 + e of tile t stand in quarter q4 of a wave, so these sixteen
+// follow with a pass of their own.  (681 tokens of eight requests, 8 KV heads, 380 to 849 blocks: 22.7 us.)  The products of rows 4 q4 + e of tile t stand in quarter q4 of a wave, so these sixteen
 // are the heads of 16 / G whole tokens, one after the other, and a token's largest is found in registers.
 constexpr int kTiles = 4;
 
@@ -283,11 +284,14 @@ __global__ __launch_bounds__(256) void score_group_kernel(Geom g, SelectArgs a)
     typedef BoundsTile<kD> Tile;
     __shared__ __attribute__((aligned(256))) char s_tile[4][2][Tile::kBytes];
     __shared__ int32_t s_row[kScoreBlocks], s_exp[kScoreBlocks];
-    const int item = a.parts(blockIdx.x), part = blockIdx.x - item * a.score_parts, group = a.heads(item), kvh = item - group * g.Hkv;
+    const int part = a.parts(blockIdx.x), item = blockIdx.x - part * (int)a.parts.by, group = a.heads(item), kvh = item - group * g.Hkv;
     const int n0 = a.n0 + group * a.group_tokens, n1 = min(n0 + a.group_tokens, a.n0 + a.n_tokens);
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, q4 = lane >> 4;
     const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)s_tile[w][0];
     auto tile = [&](int k) { return Tile{ring + (uint32_t)(k & 1) * Tile::kBytes}; };
+    // lane l looks up the group's token l, and what it chooses from
+    int seq_l = -1, pos_l = 0;
+    if (lane < n1 - n0 && !token_place(a.token_seq, a.token_pos, n0 + lane, a.B, a.max_blocks, seq_l, pos_l)) seq_l = -1;
     __shared__ __attribute__((aligned(16))) int8_t s_q[kTiles][16 * 2 * kD];
     __shared__ __attribute__((aligned(16))) float s_scale[kTiles][16];
     const int of_group = a.group_tokens / 4;             // tokens of a quarter
@@ -303,9 +307,6 @@ __global__ __launch_bounds__(256) void score_group_kernel(Geom g, SelectArgs a)
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) q[t] = QueryTile<kBf16, kD>{s_q[t], s_scale[t]}.operands(r16, q4);
     const char *digests = (const char *)a.digests + digest_rows(g, a, kvh) * (2 * kD);
-    // lane l looks up the group's token l, and what it chooses from
-    int seq_l = -1, pos_l = 0;
-    if (lane < n1 - n0 && !token_place(a.token_seq, a.token_pos, n0 + lane, a.B, a.max_blocks, seq_l, pos_l)) seq_l = -1;
     const Window win_l(seq_l >= 0 ? pos_l : 0, a.n_sink, a.n_local);
     const bool scores_l = seq_l >= 0 && win_l.candidates() > a.n_top;
     for (int t0 = n0, t1; t0 < n1; t0 = t1) {
@@ -710,7 +711,7 @@ static hipError_t launch_scores(const Geom &g, SelectArgs a, const Launch &L)
     a.score_parts = (a.max_blocks + kScoreBlocks - 1) / kScoreBlocks;
     const int64_t grid = (int64_t)((a.n_tokens + a.group_tokens - 1) / a.group_tokens) * g.Hkv * a.score_parts;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
-    a.parts = FastDiv((uint32_t)a.score_parts);
+    a.parts = FastDiv((uint32_t)(grid / a.score_parts));
     if (grouped) TC_LAUNCH((score_group_kernel<kBf16, kD>), (unsigned)grid, 0, L, g, a);
     else TC_LAUNCH((score_token_kernel<kBf16, kD>), (unsigned)grid, 0, L, g, a);
     return hipGetLastError();

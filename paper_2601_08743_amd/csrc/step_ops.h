@@ -65,7 +65,7 @@ struct SelectArgs {
     int64_t score_stride;
     int32_t n0, n_tokens, layer, B, max_blocks, n_sink, n_top, n_local, first_block;    // tokens n0 .. n0 + n_tokens - 1
     int32_t score_parts, group_tokens;        // scores: work-groups along the candidates, and tokens of one
-    FastDiv heads, parts;                     // KV heads, score_parts
+    FastDiv heads, parts;                     // KV heads, work-groups of one range of the candidates
 };
 
 struct BlockAttnArgs {
