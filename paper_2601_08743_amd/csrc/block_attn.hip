@@ -379,9 +379,9 @@ __device__ __forceinline__ void write_fixed(const SelectArgs &a, const Window &w
 // out take two).  A thread holds kPer neighbouring candidates, so that one prefix sum over the threads places them.
 constexpr int kSelectBins = 1024;
 
-template <int kThreads>
+template <int kThreads, int kBins>
 struct PickShared {
-    __attribute__((aligned(16))) uint32_t bins[kSelectBins], lo[kThreads / 64], hi[kThreads / 64], wave[kThreads / 64], found[3];
+    __attribute__((aligned(16))) uint32_t bins[kBins], lo[kThreads / 64], hi[kThreads / 64], wave[kThreads / 64], found[3];
 };
 
 // The sum of the waves' values before wave w.
@@ -394,16 +394,17 @@ __device__ __forceinline__ uint32_t before_wave(const uint32_t (&wave)[kWaves], 
     return sum;
 }
 
-// key: of candidates c0 .. c0 + kPer - 1 (of `cand`, at most 65535); s.bins are zero, in all threads' sight.
-template <int kThreads, int kPer>
-__device__ __forceinline__ void pick(PickShared<kThreads> &s, const uint32_t (&key)[kPer], int c0, int cand, int n_top, int first, int32_t *list, int tid)
+// key: of `have` candidates from c0 on (of 65535 at most in all threads); s.bins are zero, in all threads' sight.
+template <int kThreads, int kAll, int kPer>
+__device__ __forceinline__ void pick(PickShared<kThreads, kAll> &s, const uint32_t (&key)[kPer], int c0, int have, int n_top, int first, int32_t *list, int tid)
 {
-    constexpr int kBins = kSelectBins / kThreads;
+    constexpr int kBins = kAll / kThreads;               // of a thread
+    constexpr int kBits = __builtin_ctz(kAll);
     const int lane = tid & 63, w = tid >> 6;
     uint32_t lo = 0xffffffffu, hi = 0;
 #pragma unroll
     for (int k = 0; k < kPer; ++k)
-        if (c0 + k < cand) {
+        if (k < have) {
             lo = min(lo, key[k]);
             hi = max(hi, key[k]);
         }
@@ -417,24 +418,24 @@ __device__ __forceinline__ void pick(PickShared<kThreads> &s, const uint32_t (&k
     uint32_t want = n_top;
     bool whole = false;
     while (lo < hi) {
-        const int shift = max(0, 22 - (int)__builtin_clz(hi - lo));     // (hi - lo) >> shift < 1024
+        const int shift = max(0, 32 - kBits - (int)__builtin_clz(hi - lo));     // (hi - lo) >> shift < kAll
 #pragma unroll
         for (int k = 0; k < kPer; ++k)
-            if (c0 + k < cand && key[k] >= lo && key[k] <= hi) atomicAdd(&s.bins[(key[k] - lo) >> shift], 1u);
+            if (k < have && key[k] >= lo && key[k] <= hi) atomicAdd(&s.bins[(key[k] - lo) >> shift], 1u);
         __syncthreads();
-        // counted from the top: thread t holds bins 1023 - kBins t and the next lower ones
+        // counted from the top: thread t holds bins kAll - 1 - kBins t and the next lower ones
         uint32_t c[kBins], sum = 0;
 #pragma unroll
-        for (int k = 0; k < kBins; ++k) { c[k] = s.bins[kSelectBins - 1 - kBins * tid - k]; sum += c[k]; }
+        for (int k = 0; k < kBins; ++k) { c[k] = s.bins[kAll - 1 - kBins * tid - k]; sum += c[k]; }
         const uint32_t x = wave_prefix(sum);
         if (lane == 63) s.wave[w] = x;
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < kBins; ++k) s.bins[kSelectBins - 1 - kBins * tid - k] = 0;
+        for (int k = 0; k < kBins; ++k) s.bins[kAll - 1 - kBins * tid - k] = 0;
         uint32_t above = before_wave(s.wave, w) + x - sum;
 #pragma unroll
         for (int k = 0; k < kBins; ++k) {
-            if (above < want && above + c[k] >= want) { s.found[0] = kSelectBins - 1 - kBins * tid - k; s.found[1] = above; s.found[2] = c[k]; }
+            if (above < want && above + c[k] >= want) { s.found[0] = kAll - 1 - kBins * tid - k; s.found[1] = above; s.found[2] = c[k]; }
             above += c[k];
         }
         __syncthreads();
@@ -448,8 +449,8 @@ __device__ __forceinline__ void pick(PickShared<kThreads> &s, const uint32_t (&k
     uint32_t mine = 0;                                   // (keys at the threshold << 16) + keys above it
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
-        const bool have = c0 + k < cand;
-        mine += have && (whole ? key[k] >= lo : key[k] > lo) ? 1u : have && !whole && key[k] == lo ? 0x10000u : 0u;
+        const bool is = k < have;
+        mine += is && (whole ? key[k] >= lo : key[k] > lo) ? 1u : is && !whole && key[k] == lo ? 0x10000u : 0u;
     }
     const uint32_t x = wave_prefix(mine);
     if (lane == 63) s.wave[w] = x;                       // (its last reads were before the loop's last barrier)
@@ -458,20 +459,25 @@ __device__ __forceinline__ void pick(PickShared<kThreads> &s, const uint32_t (&k
     uint32_t above = before & 0xffffu, ties = before >> 16;
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
-        const bool have = c0 + k < cand, over = have && (whole ? key[k] >= lo : key[k] > lo), tie = have && !whole && key[k] == lo;
+        const bool is = k < have, over = is && (whole ? key[k] >= lo : key[k] > lo), tie = is && !whole && key[k] == lo;
         if (over || (tie && ties < want)) list[first + above + min(ties, want)] = first + c0 + k;
         above += over;
         ties += tie;
     }
 }
 
-// Lists from scores in memory: a work-group a (token, KV head), a thread kSelectPer candidates.  A chain of barriers: 5.6 us for 32
-// work-groups (118 of 1.7 k), 19 for 5.4 k (60 of some 600).
-constexpr int kSelectPer = 8, kSelectFew = 256 * kSelectPer;
+// Lists from scores in memory: a work-group a (token, KV head).
+//   kThreads 256: eight candidates a thread, 1024 bins, a chain of barriers (32 items, 118 of 1.7 k each: 5.6 us)
+//   kThreads 64: a wave, which waits for no other, up to 16 a thread, 256 bins.  Longer from start to end, but beyond four waves a CU
+//   what counts is what they do together (5.4 k items, 60 of some 600: 14.2 us, 17.6 by 256 threads; a pass of scores, list and
+//   attention for 640 items 41.0 against 39.6, for 1088 50.0 against 50.5, for 15 k 325 against 341)
+constexpr int kSelectWave = 64 * 16, kSelectFew = 256 * 8;              // table entries that each does for
+constexpr int kSelectItems = 1024;
 
-__global__ __launch_bounds__(256) void select_kernel(Geom g, SelectArgs a)
+template <int kThreads, int kPer, int kBins>
+__global__ __launch_bounds__(kThreads) void select_kernel(Geom g, SelectArgs a)
 {
-    __shared__ PickShared<256> s;
+    __shared__ PickShared<kThreads, kBins> s;
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(4)));
     const int token = a.heads(blockIdx.x), n = a.n0 + token, kvh = blockIdx.x - token * g.Hkv, tid = threadIdx.x;
     int seq, pos;
@@ -481,12 +487,13 @@ __global__ __launch_bounds__(256) void select_kernel(Geom g, SelectArgs a)
     int32_t *list = a.lists + ((int64_t)n * g.Hkv + kvh) * (a.n_sink + a.n_top + a.n_local);
     if (cand > a.n_top && a.n_top > 0) {
         const uint32_t *scores = a.scores + ((int64_t)(n - a.n0) * g.Hkv + kvh) * a.score_stride + win.first;
-        const int c0 = kSelectPer * tid;
-        uint32_t key[kSelectPer];
+        const int per = (cand + 4 * kThreads - 1) / (4 * kThreads) * 4, c0 = per * tid;
+        uint32_t key[kPer];
 #pragma unroll
-        for (int k = 0; k < kSelectPer; k += 4) {
+        for (int k = 0; k < kPer; k += 4) {
             u32x4 v = {0, 0, 0, 0};
-            if (c0 + k + 3 < cand) v = *(const u32x4 *)(scores + c0 + k);
+            if (k >= per) {                              // (the same for all)
+            } else if (c0 + k + 3 < cand) v = *(const u32x4 *)(scores + c0 + k);
             else if (c0 + k < cand) {                    // (the row's last few)
                 v[0] = scores[c0 + k];
                 v[1] = c0 + k + 1 < cand ? scores[c0 + k + 1] : 0;
@@ -495,10 +502,11 @@ __global__ __launch_bounds__(256) void select_kernel(Geom g, SelectArgs a)
 #pragma unroll
             for (int e = 0; e < 4; ++e) key[k + e] = v[e];
         }
+        static_assert(kBins == 4 * kThreads, "a thread clears four bins");
         *(uint4 *)&s.bins[4 * tid] = make_uint4(0, 0, 0, 0);             // (seen behind pick's first barrier)
-        pick<256>(s, key, c0, cand, a.n_top, win.first, list, tid);
+        pick(s, key, c0, min(max(cand - c0, 0), per), a.n_top, win.first, list, tid);
     }
-    write_fixed(a, win, list, tid, 256);
+    write_fixed(a, win, list, tid, kThreads);
 }
 
 // The same for tables of more than kSelectFew entries: the scores stay in memory and are read again in every round.
@@ -611,7 +619,7 @@ template <bool kBf16, int kD>
 __global__ __launch_bounds__(1024) void score_select_kernel(Geom g, SelectArgs a)
 {
     extern __shared__ __attribute__((aligned(256))) char s_ring[];       // two tiles a wave
-    __shared__ PickShared<1024> s_pick;
+    __shared__ PickShared<1024, kSelectBins> s_pick;
     __shared__ int32_t s_row[kFusedBlocks];
     __shared__ float s_prod[kFusedBlocks];
     const int token = a.heads(blockIdx.x), n = a.n0 + token, kvh = blockIdx.x - token * g.Hkv;
@@ -685,7 +693,7 @@ __global__ __launch_bounds__(1024) void score_select_kernel(Geom g, SelectArgs a
 #pragma unroll
     for (int k = 0; k < 2; ++k)
         if (c0 + k < cand) key[k] = BlockScale(exponent[k]).key(s_prod[c0 + k]);
-    pick<1024>(s_pick, key, c0, cand, a.n_top, win.first, list, tid);
+    pick(s_pick, key, c0, min(cand - c0, 2), a.n_top, win.first, list, tid);
     write_fixed(a, win, list, tid, 1024);                // (last: a barrier behind a store to memory waits for it)
 }
 
@@ -732,7 +740,8 @@ hipError_t launch_select(const Geom &g, SelectArgs a, const Launch &L)
                            : g.D == 64 ? launch_scores<false, 64>(g, a, L) : launch_scores<false, 128>(g, a, L);
         if (e != hipSuccess) return e;
     }
-    if (most <= kSelectFew) TC_LAUNCH(select_kernel, (unsigned)items, 0, L, g, a);
+    if (most <= kSelectWave && items > kSelectItems) TC_LAUNCH_N((select_kernel<64, 16, 256>), (unsigned)items, 64, 0, L, g, a);
+    else if (most <= kSelectFew) TC_LAUNCH_N((select_kernel<256, 8, kSelectBins>), (unsigned)items, 256, 0, L, g, a);
     else TC_LAUNCH(select_long_kernel, (unsigned)items, 0, L, g, a);
     return hipGetLastError();
 }

@@ -194,6 +194,23 @@ def test_lists_over_tables_of_some_thousand_blocks(hq, hkv, d, dtype, max_blocks
     pool.close()
 
 
+@pytest.mark.parametrize("max_blocks", [257, 1024, 1025])
+def test_lists_of_many_tokens_over_long_tables(max_blocks):
+    """More than a thousand lists, from every number of candidates; few different blocks, so scores are tied."""
+    pool = SH.Pool(8, 8, 128, "bf16", 90)
+    pool.fill(6)
+    table = np.random.default_rng(max_blocks).integers(0, 90, size=(2, max_blocks))
+    table[1, 3:50:9] = -1
+    digests = _digested(pool, np.arange(90))
+    seq = [0] * 70 + [1] * 71
+    pos = [int(x) for x in np.linspace(0, 16 * max_blocks - 1, 70)] + [int(x) for x in np.linspace(16 * 7, 16 * max_blocks - 1, 71)]
+    q = pool.rows(len(seq), 8, 3)
+    for sink, top, local in ((0, 1, 1), (2, 100, 3)):
+        got = _lists(pool, q, seq, pos, table, digests, sink, top, local)
+        np.testing.assert_array_equal(got, _want_lists(pool, q, seq, pos, table, digests, sink, top, local))
+    pool.close()
+
+
 def test_lists_do_not_depend_on_the_workspace():
     pool = SH.Pool(8, 2, 128, "bf16", 120)
     pool.fill(1)
