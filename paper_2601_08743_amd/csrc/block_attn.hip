@@ -806,17 +806,19 @@ __device__ __forceinline__ ListUnit list_unit(const Geom &g, const BlockAttnArgs
 // from there: loaded straight into the operands' registers, where neighbouring lanes are neighbouring rows of 256 bytes, keys take a
 // CU's address path 64 cycles a kilobyte instead of 16.  The next unit's keys are requested as soon as this one's are in
 // registers, and so the values.  (Values straight to registers, 32-byte rows, and twice the waves: slower for every list tried.)
-// Bound: 53 blocks for each of 4 items, 7.5 us, the chain of units; 49 for each of 128, 51 MB, 11.1 us = 4.6 TB/s, what a CU takes from
+// Bound: 53 blocks for each of 4 items, 7.7 us, the chain of units; 49 for each of 128, 51 MB, 11.1 us = 4.6 TB/s, what a CU takes from
 // memory; 64 for each of 5.4 k items, 157 us, the L2's 2.8 GB = 18 TB/s, of which a fifth comes from further (all there: 105 us).
 constexpr int kBaRow = 132;                              // padded output row of the exchange (floats), maximum and sum behind it
 constexpr int kBaBlock = 4096;                           // one head's K (or V) in one block
+constexpr int kBaWaves = 4;
 constexpr int kBaWave = 4 * kBaBlock;                    // K of a unit: rows of 256 bytes, 16-byte chunk c of row r at c ^ r; V: two blocks verbatim
 
 constexpr float kBaRescale = 8.f;                        // weights grow to 2^8 before the reference moves
 
-template <int kWaves, bool kSplit>
-__global__ __launch_bounds__(64 * kWaves, 2) void block_attn_bf16_kernel(Geom g, BlockAttnArgs a)
+template <bool kSplit>
+__global__ __launch_bounds__(64 * kBaWaves, 2) void block_attn_bf16_kernel(Geom g, BlockAttnArgs a)
 {
+    constexpr int kWaves = kBaWaves;
     extern __shared__ __attribute__((aligned(256))) char lds[];          // (the XOR addressing of the K rows needs them 256-byte aligned)
     const int chunks = (int)a.chunks.by;
     const int item = a.splits(blockIdx.x), split = blockIdx.x - item * a.n_splits;
@@ -1113,17 +1115,17 @@ __global__ __launch_bounds__(256) void block_merge_kernel(Geom g, BlockAttnArgs 
     }
 }
 
-// Waves of a work-group and ranges of a list.
-//   bf16: a work-group of eight waves reads a list at what a CU takes from memory, some 80 GB/s, so ranges for work-groups of their own
-//   pay for the launch that combines them (4 us with the gap) only beyond kBaRounds units a wave: 128 blocks for each of 32
-//   items 8.7 + 3.6 us in 4 ranges, 15.2 in one; 53 blocks for each of 4 items 7.5 in one, 5.5 + 4.1 in 7.  Items that fill the chip:
-//   four waves, two work-groups a CU, whose starts and ends overlap (5.4 k items of 64 blocks: 157 us; with eight waves 205).
+// Ranges of a list.  Four waves to a work-group: two of them share a CU where items fill the chip, and their starts and ends overlap
+// (5.4 k bf16 items of 64 blocks: 157 us; with eight waves 205), and for few items eight waves are no faster.
+//   bf16: a work-group reads a list at what a CU takes from memory, some 80 GB/s, so ranges of eight units, two a wave, for work-groups of
+//   their own pay for the launch that combines them (4 us with the gap) where lists are long and few: a pass of scores, list and attention
+//   takes, in ranges and in one, for 8 lists of 80 blocks 13.6 and 15.6 us, of 160 14.7 and 21.2; for 32 of 80 15.2 and 16.8, of 128
+//   17.5 and 21.2; for 48 of 80 17.1 and 17.3, of 160 22.4 and 24.4; for 64 of 160 25.7 and 24.9; for 8 of 44 13.5 and 13.4.
 //   fp32: bound by its own vector work, 400 instructions a block of four rows, so a unit a wave up to two work-groups a CU (24 blocks
 //   for each of 20 items 5.3 + 2.8 us; in one range of eight waves 9.8).
-constexpr int kBaRounds = 6;
+constexpr int kBaRangeItems = 48, kBaRangeUnits = 28;
 
-struct BaShape { int waves, splits; };
-static BaShape block_attn_shape(int Hq, int Hkv, int esize, int n_tokens, int n_list)
+int block_attn_splits(int Hq, int Hkv, int esize, int n_tokens, int n_list)
 {
     const int G = Hq / Hkv, rows = esize == 2 ? 16 : kBaF32Rows;
     const int64_t items = std::max<int64_t>((int64_t)n_tokens * Hkv * ((G + rows - 1) / rows), 1);
@@ -1131,14 +1133,8 @@ static BaShape block_attn_shape(int Hq, int Hkv, int esize, int n_tokens, int n_
     auto ranges = [&](int64_t most, int64_t at_least) {  // up to `most` work-groups, none with fewer units
         return (int)std::max<int64_t>(1, std::min<int64_t>({most / items, (units + at_least - 1) / at_least, 32}));
     };
-    if (esize != 2) return BaShape{4, ranges(512, 4)};
-    if (items > 256 || units <= 4) return BaShape{4, 1};
-    return BaShape{8, units <= 8 * kBaRounds || items > 128 ? 1 : ranges(256, 16)};
-}
-
-int block_attn_splits(int Hq, int Hkv, int esize, int n_tokens, int n_list)
-{
-    return block_attn_shape(Hq, Hkv, esize, n_tokens, n_list).splits;
+    if (esize != 2) return ranges(512, 4);
+    return items > kBaRangeItems || units <= kBaRangeUnits ? 1 : ranges(256, 8);
 }
 
 int block_attn_parts(int Hq, int Hkv, int esize, int n_tokens, int n_list)
@@ -1158,16 +1154,15 @@ static hipError_t launch_attn_f32(const Geom &g, const BlockAttnArgs &a, unsigne
     return hipGetLastError();
 }
 
-template <int kWaves, bool kSplit>
-static hipError_t launch_attn_bf16_waves(const Geom &g, const BlockAttnArgs &a, unsigned grid, const Launch &L)
+template <bool kSplit>
+static hipError_t launch_attn_bf16(const Geom &g, const BlockAttnArgs &a, unsigned grid, const Launch &L)
 {
     static PerDeviceOnce configured;
     const hipError_t e = configured.run([] {
-        return hipFuncSetAttribute((const void *)block_attn_bf16_kernel<kWaves, kSplit>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                   kWaves * kBaWave);
+        return hipFuncSetAttribute((const void *)block_attn_bf16_kernel<kSplit>, hipFuncAttributeMaxDynamicSharedMemorySize, kBaWaves * kBaWave);
     });
     if (e != hipSuccess) return e;
-    TC_LAUNCH_N((block_attn_bf16_kernel<kWaves, kSplit>), grid, 64 * kWaves, kWaves * kBaWave, L, g, a);
+    TC_LAUNCH_N(block_attn_bf16_kernel<kSplit>, grid, 64 * kBaWaves, kBaWaves * kBaWave, L, g, a);
     return hipGetLastError();
 }
 
@@ -1181,11 +1176,8 @@ hipError_t launch_block_attn(const Geom &g, BlockAttnArgs a, const Launch &L)
     a.chunks = FastDiv((uint32_t)chunks);
     a.heads = FastDiv((uint32_t)g.Hkv);
     const bool split = a.n_splits > 1;
-    const int waves = block_attn_shape(g.Hq, g.Hkv, g.esize, a.n_tokens, a.n_list).waves;
     const unsigned n = (unsigned)grid;
-    if (g.esize == 2)
-        return split ? launch_attn_bf16_waves<8, true>(g, a, n, L)
-             : waves == 8 ? launch_attn_bf16_waves<8, false>(g, a, n, L) : launch_attn_bf16_waves<4, false>(g, a, n, L);
+    if (g.esize == 2) return split ? launch_attn_bf16<true>(g, a, n, L) : launch_attn_bf16<false>(g, a, n, L);
     if (g.D == 64) return split ? launch_attn_f32<64, true>(g, a, n, L) : launch_attn_f32<64, false>(g, a, n, L);
     return split ? launch_attn_f32<128, true>(g, a, n, L) : launch_attn_f32<128, false>(g, a, n, L);
 }
