@@ -718,12 +718,14 @@ static hipError_t launch_scores(const Geom &g, SelectArgs a, const Launch &L)
     a.group_tokens = grouped ? 4 * (16 / g.G) : 1;
     a.score_parts = (a.max_blocks + kScoreBlocks - 1) / kScoreBlocks;
     const int64_t grid = (int64_t)((a.n_tokens + a.group_tokens - 1) / a.group_tokens) * g.Hkv * a.score_parts;
-    if (grid > INT32_MAX) return hipErrorInvalidValue;
+    if (grid > kStepMaxGroups) return hipErrorInvalidValue;
     a.parts = FastDiv((uint32_t)(grid / a.score_parts));
     if (grouped) TC_LAUNCH((score_group_kernel<kBf16, kD>), (unsigned)grid, 0, L, g, a);
     else TC_LAUNCH((score_token_kernel<kBf16, kD>), (unsigned)grid, 0, L, g, a);
     return hipGetLastError();
 }
+
+int64_t select_groups(int Hkv, int max_blocks) { return (int64_t)Hkv * std::max(1, (max_blocks + kScoreBlocks - 1) / kScoreBlocks); }
 
 hipError_t launch_select(const Geom &g, SelectArgs a, const Launch &L)
 {
@@ -731,7 +733,7 @@ hipError_t launch_select(const Geom &g, SelectArgs a, const Launch &L)
     a.heads = FastDiv((uint32_t)g.Hkv);
     const int most = a.max_blocks;                       // candidates of any token
     const int64_t items = (int64_t)a.n_tokens * g.Hkv;
-    if (items > INT32_MAX) return hipErrorInvalidValue;
+    if (items > kStepMaxGroups) return hipErrorInvalidValue;
     if (most <= kFusedBlocks && items <= kFusedItems)
         return g.esize == 2 ? launch_score_select<true, 128>(g, a, L)
              : g.D == 64 ? launch_score_select<false, 64>(g, a, L) : launch_score_select<false, 128>(g, a, L);
@@ -1125,10 +1127,16 @@ __global__ __launch_bounds__(256) void block_merge_kernel(Geom g, BlockAttnArgs 
 //   for each of 20 items 5.3 + 2.8 us; in one range of eight waves 9.8).
 constexpr int kBaRangeItems = 48, kBaRangeUnits = 28;
 
-int block_attn_splits(int Hq, int Hkv, int esize, int n_tokens, int n_list)
+// 16 rows of a token and KV head, or 8, to a work-group
+int block_attn_groups(int Hq, int Hkv, int esize)
 {
     const int G = Hq / Hkv, rows = esize == 2 ? 16 : kBaF32Rows;
-    const int64_t items = std::max<int64_t>((int64_t)n_tokens * Hkv * ((G + rows - 1) / rows), 1);
+    return Hkv * ((G + rows - 1) / rows);
+}
+
+int block_attn_splits(int Hq, int Hkv, int esize, int n_tokens, int n_list)
+{
+    const int64_t items = std::max<int64_t>((int64_t)n_tokens * block_attn_groups(Hq, Hkv, esize), 1);
     const int units = esize == 2 ? (n_list + 1) / 2 : n_list;
     auto ranges = [&](int64_t most, int64_t at_least) {  // up to `most` work-groups, none with fewer units
         return (int)std::max<int64_t>(1, std::min<int64_t>({most / items, (units + at_least - 1) / at_least, 32}));
@@ -1169,9 +1177,9 @@ static hipError_t launch_attn_bf16(const Geom &g, const BlockAttnArgs &a, unsign
 hipError_t launch_block_attn(const Geom &g, BlockAttnArgs a, const Launch &L)
 {
     if (a.n_tokens == 0) return hipSuccess;
-    const int rows = g.esize == 2 ? 16 : kBaF32Rows, chunks = (g.G + rows - 1) / rows;
-    const int64_t grid = (int64_t)a.n_tokens * g.Hkv * chunks * a.n_splits;
-    if (grid > INT32_MAX) return hipErrorInvalidValue;
+    const int groups = block_attn_groups(g.Hq, g.Hkv, g.esize), chunks = groups / g.Hkv;
+    const int64_t grid = (int64_t)a.n_tokens * groups * a.n_splits;
+    if (grid > kStepMaxGroups) return hipErrorInvalidValue;
     a.splits = FastDiv((uint32_t)a.n_splits);
     a.chunks = FastDiv((uint32_t)chunks);
     a.heads = FastDiv((uint32_t)g.Hkv);
@@ -1186,7 +1194,7 @@ hipError_t launch_block_merge(const Geom &g, const BlockAttnArgs &a, const Launc
 {
     if (a.n_tokens == 0) return hipSuccess;
     const int64_t rows = (int64_t)a.n_tokens * g.Hq, per = 256 / (g.D / 4), blocks = (rows + per - 1) / per;
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    if (blocks > kStepMaxGroups) return hipErrorInvalidValue;
     if (g.esize == 2) TC_LAUNCH((block_merge_kernel<true, 128>), (unsigned)blocks, 0, L, g, a);
     else if (g.D == 64) TC_LAUNCH((block_merge_kernel<false, 64>), (unsigned)blocks, 0, L, g, a);
     else TC_LAUNCH((block_merge_kernel<false, 128>), (unsigned)blocks, 0, L, g, a);

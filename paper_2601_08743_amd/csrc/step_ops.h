@@ -10,6 +10,7 @@ namespace tc {
 constexpr int kStepMaxSeqs = 8192;            // requests of a step: three integers of each are kept in LDS
 constexpr int kStepMaxTokens = 1 << 20;       // tokens of a step: their sum over the requests stays below 2^34
 constexpr int kRopeMaxAxes = 4;
+constexpr int64_t kStepMaxGroups = (1 << 24) - 1;       // work-groups of 256 in a launch, whose grid counts threads in 32 bits
 
 // Division of 0 <= n < 2^31 by a number fixed at the launch: a multiplication and a shift (scalar ones, where n is the same for a
 // wave; a division proper is a hundred cycles at the start of every short kernel).
@@ -148,6 +149,9 @@ __device__ __forceinline__ void turn_chunk(uint4 &x, uint4 &y, const float2 *w)
 int block_attn_splits(int Hq, int Hkv, int esize, int n_tokens, int n_list);
 // The most (token, range) partials of a query head that up to n_tokens tokens keep, where lists are shared out.
 int block_attn_parts(int Hq, int Hkv, int esize, int n_tokens, int n_list);
+// Work-groups that a token's lists, and its attention in one range, take in a launch.
+int64_t select_groups(int Hkv, int max_blocks);
+int block_attn_groups(int Hq, int Hkv, int esize);
 
 hipError_t launch_step_tables(const StepTables &s, const Launch &L);
 hipError_t launch_rope_append(const Geom &g, const RopeAppend &a, const Launch &L);

@@ -401,7 +401,7 @@ hipError_t launch_digest(const Geom &g, DigestArgs a, int l1, const Launch &L)
 {
     if (a.n == 0 || l1 <= a.l0) return hipSuccess;
     const int64_t units = (int64_t)a.n * g.Hkv;
-    if (units > INT32_MAX - 3) return hipErrorInvalidValue;
+    if ((units + 3) / 4 > kStepMaxGroups) return hipErrorInvalidValue;
     a.heads = FastDiv((uint32_t)g.Hkv);
     const dim3 grid((unsigned)((units + 3) / 4), l1 - a.l0);
     if (g.esize == 2) TC_LAUNCH((digest_kernel<true, 16>), grid, 0, L, g, a);

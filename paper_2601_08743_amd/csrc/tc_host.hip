@@ -1263,7 +1263,11 @@ tc_status tc_digest_blocks(tc_ctx *ctx, int32_t l0, int32_t l1, const int32_t *e
     a.entries = entries; a.digests = (int8_t *)digests; a.n = n; a.l0 = l0;
     a.exps_at = (int64_t)ctx->cfg.n_layers * ctx->cfg.n_kv_heads * ctx->cfg.n_pool_blocks * 2 * ctx->cfg.head_dim;
     a.first_block = (int32_t)first_pool_block(ctx->cfg);
-    TC_HIP(ctx, launch_digest(ctx->geom, a, l1, Launch{stream, nullptr, nullptr}));
+    const int32_t at_once = (int32_t)std::max<int64_t>(4 * kStepMaxGroups / ctx->cfg.n_kv_heads, 1);
+    for (int32_t left = n; left > 0; left -= a.n, a.entries += a.n) {
+        a.n = std::min(left, at_once);
+        TC_HIP(ctx, launch_digest(ctx->geom, a, l1, Launch{stream, nullptr, nullptr}));
+    }
     slots_read(ctx, stream);
     return TC_OK;
 }
@@ -1290,7 +1294,7 @@ tc_status tc_select_blocks(tc_ctx *ctx, int32_t layer, const void *q, const int3
     a.scores = (uint32_t *)workspace; a.score_stride = max_blocks;
     a.layer = layer; a.B = B; a.max_blocks = max_blocks; a.n_sink = n_sink; a.n_top = n_top; a.n_local = n_local;
     a.first_block = (int32_t)first_pool_block(ctx->cfg);
-    int64_t round = n_tokens;
+    int64_t round = std::min<int64_t>(n_tokens, std::max<int64_t>(kStepMaxGroups / select_groups(ctx->cfg.n_kv_heads, max_blocks), 1));
     if (max_blocks > n_top && n_top > 0) {               // else every candidate is listed, or none
         const size_t one = score_bytes_per_token(ctx->cfg, max_blocks);
         if (!workspace || workspace_bytes < one)
@@ -1333,7 +1337,14 @@ tc_status tc_block_attn(tc_ctx *ctx, int32_t layer, const void *q, const int32_t
     a.first_block = (int32_t)first_pool_block(ctx->cfg);
     a.part_o = (float *)workspace;
     if (need > 0) a.part_ml = a.part_o + (size_t)n_tokens * g.Hq * splits * g.D;
-    TC_HIP(ctx, timed_launch(ctx, 2, stream, [&](const Launch &ln) { return launch_block_attn(ctx->geom, a, ln); }));
+    const int32_t at_once = (int32_t)std::max<int64_t>(kStepMaxGroups / ((int64_t)block_attn_groups(g.Hq, g.Hkv, g.esize) * splits), 1);
+    for (int32_t left = n_tokens; left > 0; left -= a.n_tokens) {        // (more than one launch only of lists in one range)
+        a.n_tokens = std::min(left, at_once);
+        TC_HIP(ctx, timed_launch(ctx, 2, stream, [&](const Launch &ln) { return launch_block_attn(ctx->geom, a, ln); }));
+        if (left == a.n_tokens) break;
+        a.q += (int64_t)a.n_tokens * g.Hq * g.head_bytes; a.out += (int64_t)a.n_tokens * g.Hq * g.head_bytes;
+        a.lists += (int64_t)a.n_tokens * g.Hkv * n_list; a.token_seq += a.n_tokens; a.token_pos += a.n_tokens;
+    }
     if (a.n_splits > 1) TC_HIP(ctx, timed_launch(ctx, 3, stream, [&](const Launch &ln) { return launch_block_merge(ctx->geom, a, ln); }));
     slots_read(ctx, stream);
     return TC_OK;

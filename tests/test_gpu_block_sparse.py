@@ -385,6 +385,36 @@ def test_attention_with_extreme_values(dtype, d):
     pool.close()
 
 
+def test_the_largest_number_of_tokens():
+    """2^20 tokens of 17 KV heads are more work-groups than one launch takes; all but some at both ends are padded rows, which
+    stay as they are."""
+    pool = SH.Pool(17, 17, 64, "f32", 12)
+    pool.fill(5)
+    n, few = 1 << 20, [0, 1, (1 << 24) // 17 - 1, (1 << 24) // 17, (1 << 24) // 17 + 1, (1 << 20) - 2, (1 << 20) - 1]
+    at = torch.tensor(few, device="cuda")
+    table = SH.i32(np.arange(12)[None])
+    digests = _digested(pool, np.arange(12))
+    seq, pos = SH.i32(np.full(n, -1)), SH.i32(np.full(n, 190))
+    seq[at] = 0
+    q = torch.zeros((n, 17, 64), device="cuda")
+    q[at] = pool.rows(len(few), 17, 3)
+    lists, out = torch.full((n, 17, 3), -99, dtype=torch.int32, device="cuda"), torch.full((n, 17, 64), 7.0, device="cuda")
+    ws = pool.workspace(n, 12, 3)
+    pool.ctx.tc_select_blocks(0, q, seq, pos, table, digests, 1, 1, 1, lists, ws)
+    pool.ctx.tc_block_attn(0, q, seq, pos, table, lists, out, 0.1, ws)
+    few_lists = torch.full((len(few), 17, 3), -99, dtype=torch.int32, device="cuda")
+    few_out = torch.full((len(few), 17, 64), 7.0, device="cuda")
+    pool.ctx.tc_select_blocks(0, q[at], seq[at], pos[at], table, digests, 1, 1, 1, few_lists, ws)
+    pool.ctx.tc_block_attn(0, q[at], seq[at], pos[at], table, few_lists, few_out, 0.1, ws)
+    torch.cuda.synchronize()
+    want = _want_lists(pool, q[at], [0] * len(few), [190] * len(few), np.arange(12)[None], digests, 1, 1, 1)
+    np.testing.assert_array_equal(few_lists.cpu().numpy(), want)
+    assert torch.equal(lists[at], few_lists) and torch.equal(out[at], few_out)      # (lists of one range in both)
+    lists[at], out[at] = -99, 7.0
+    assert bool((lists == -99).all()) and bool((out == 7.0).all())
+    pool.close()
+
+
 def test_offsets_beyond_32_bits():
     """A pool of more than 4 GiB in its last layer: the last blocks are read, digested and scored where they are."""
     pool = SH.Pool(8, 8, 128, "bf16", 72000)

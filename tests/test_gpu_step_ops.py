@@ -242,6 +242,23 @@ def test_digests_are_the_definition(hq, hkv, d, dtype):
     pool.close()
 
 
+def test_digests_of_a_table_that_is_mostly_empty():
+    """More rows than one launch takes, nearly all of them -1."""
+    pool = SH.Pool(8, 8, 128, "bf16", 6)
+    pool.fill(3)
+    n = (1 << 23) + 20
+    entries = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    for at, block in ((0, 4), ((1 << 23) - 2, 0), ((1 << 23) + 1, 5), (n - 1, 2)):
+        entries[at] = block
+    buf = pool.digests()
+    pool.ctx.tc_digest_blocks(0, 1, entries, buf)
+    whole = pool.digests()
+    pool.ctx.tc_digest_blocks(0, 1, SH.i32([0, 2, 4, 5]), whole)
+    torch.cuda.synchronize()
+    assert torch.equal(buf, whole)
+    pool.close()
+
+
 # ------------------------------------------------------------------------------------------------ refusals
 
 def test_refusals(small_pool):
