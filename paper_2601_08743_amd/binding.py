@@ -195,7 +195,8 @@ class Context:
         self._h = h
         self._addr = h.value
         self._keep = []                           # registered host KV
-        self._step = (self._addr, cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim, int(cfg.dtype == TC_BF16), tc_digest_bytes(cfg))
+        self._step = (self._addr, cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim, int(cfg.dtype == TC_BF16), tc_digest_bytes(cfg),
+                      torch.cuda.current_device())      # (where tc_create put it)
 
     def _check(self, rc: int):
         if rc != TC_OK:

@@ -59,32 +59,6 @@ const at::Tensor &tensor(PyObject *x, const char *name)
     return THPVariable_Unpack(x);
 }
 
-[[noreturn]] void refuse(const at::Tensor &t, const char *name, at::ScalarType type, at::IntArrayRef shape)
-{
-    std::string s = std::string(name) + ": expected a contiguous device tensor " + c10::toString(type) + " [";
-    for (const int64_t n : shape) s += " " + std::to_string(n);
-    s += " ], got " + std::string(c10::toString(t.scalar_type())) + " [";
-    for (const int64_t n : t.sizes()) s += " " + std::to_string(n);
-    throw Refused{s + (t.is_cuda() ? " ]" : " ] in host memory")};
-}
-
-// A contiguous tensor of this type and shape.
-void *array(PyObject *x, const char *name, at::ScalarType type, at::IntArrayRef shape)
-{
-    const at::Tensor &t = tensor(x, name);
-    if (t.scalar_type() != type || !t.is_cuda() || t.sizes() != shape || !t.is_contiguous()) refuse(t, name, type, shape);
-    return t.data_ptr();
-}
-
-// A contiguous tensor of this type and any shape.
-void *any_shape(PyObject *x, const char *name, at::ScalarType type, int64_t &numel)
-{
-    const at::Tensor &t = tensor(x, name);
-    if (t.scalar_type() != type || !t.is_cuda() || !t.is_contiguous()) refuse(t, name, type, t.sizes());
-    numel = t.numel();
-    return t.data_ptr();
-}
-
 // The length of a dimension of a tensor with so many of them (what else it has to be is checked where it is handed over).
 int64_t length(PyObject *x, const char *name, int64_t dims, int64_t dim)
 {
@@ -99,37 +73,66 @@ int32_t narrow(int64_t n, const char *name)
     return (int32_t)n;
 }
 
-// Rows [n][heads][D] that may stand apart.
-void *rows(PyObject *x, const char *name, at::ScalarType type, int64_t n, int64_t heads, int64_t d, int64_t &stride)
-{
-    const at::Tensor &t = tensor(x, name);
-    const int64_t shape[3] = {n, heads, d};
-    if (t.scalar_type() != type || !t.is_cuda() || t.sizes() != at::IntArrayRef(shape, 3) ||
-        (t.numel() > 0 && ((d > 1 && t.stride(2) != 1) || (heads > 1 && t.stride(1) != d))))
-        refuse(t, name, type, at::IntArrayRef(shape, 3));
-    stride = n > 1 ? t.stride(0) : heads * d;
-    return t.data_ptr();
-}
-
-constexpr at::ScalarType kI32 = at::kInt, kI64 = at::kLong;
-
-// What a context is made of: (address, Hq, Hkv, D, bf16, digest bytes).
+// What a context is made of: (address, Hq, Hkv, D, bf16, digest bytes, device), and the arguments of its calls.
 struct Ctx {
     void *address;
     int64_t hq, hkv, d;
     at::ScalarType type;
-    int64_t digest_bytes;
+    int64_t digest_bytes, device;
     explicit Ctx(PyObject *t)
     {
-        if (!PyTuple_Check(t) || PyTuple_GET_SIZE(t) != 6) throw Refused{"bad context"};
+        if (!PyTuple_Check(t) || PyTuple_GET_SIZE(t) != 7) throw Refused{"bad context"};
         address = ::address(PyTuple_GET_ITEM(t, 0));
         hq = integer(PyTuple_GET_ITEM(t, 1));
         hkv = integer(PyTuple_GET_ITEM(t, 2));
         d = integer(PyTuple_GET_ITEM(t, 3));
         type = integer(PyTuple_GET_ITEM(t, 4)) ? at::kBFloat16 : at::kFloat;
         digest_bytes = integer(PyTuple_GET_ITEM(t, 5));
+        device = integer(PyTuple_GET_ITEM(t, 6));
+    }
+
+    [[noreturn]] void refuse(const at::Tensor &t, const char *name, at::ScalarType type, at::IntArrayRef shape) const
+    {
+        std::string s = std::string(name) + ": expected a contiguous tensor " + c10::toString(type) + " [";
+        for (const int64_t n : shape) s += " " + std::to_string(n);
+        s += " ] on device " + std::to_string(device) + ", got " + std::string(c10::toString(t.scalar_type())) + " [";
+        for (const int64_t n : t.sizes()) s += " " + std::to_string(n);
+        throw Refused{s + (t.is_cuda() ? " ] on device " + std::to_string((int)t.get_device()) : " ] in host memory")};
+    }
+
+    bool holds(const at::Tensor &t, at::ScalarType type) const { return t.scalar_type() == type && t.is_cuda() && t.get_device() == device; }
+
+    // A contiguous tensor of this type and shape on the context's device.
+    void *array(PyObject *x, const char *name, at::ScalarType type, at::IntArrayRef shape) const
+    {
+        const at::Tensor &t = tensor(x, name);
+        if (!holds(t, type) || t.sizes() != shape || !t.is_contiguous()) refuse(t, name, type, shape);
+        return t.data_ptr();
+    }
+
+    // One of any shape.
+    void *any_shape(PyObject *x, const char *name, at::ScalarType type, int64_t &numel) const
+    {
+        const at::Tensor &t = tensor(x, name);
+        if (!holds(t, type) || !t.is_contiguous()) refuse(t, name, type, t.sizes());
+        numel = t.numel();
+        return t.data_ptr();
+    }
+
+    // Rows [n][heads][D] that may stand apart.
+    void *rows(PyObject *x, const char *name, int64_t n, int64_t heads, int64_t &stride) const
+    {
+        const at::Tensor &t = tensor(x, name);
+        const int64_t shape[3] = {n, heads, d};
+        if (!holds(t, type) || t.sizes() != at::IntArrayRef(shape, 3) ||
+            (t.numel() > 0 && ((d > 1 && t.stride(2) != 1) || (heads > 1 && t.stride(1) != d))))
+            refuse(t, name, type, at::IntArrayRef(shape, 3));
+        stride = n > 1 ? t.stride(0) : heads * d;
+        return t.data_ptr();
     }
 };
+
+constexpr at::ScalarType kI32 = at::kInt, kI64 = at::kLong;
 
 // The call itself, other Python threads running meanwhile (a launch waits where the queue is full).
 template <typename R, typename... P, typename... A>
@@ -169,11 +172,11 @@ int32_t step_tables(PyObject *const *a)
     const int64_t B = length(a[4], "block_table", 2, 0), mb = length(a[4], "block_table", 2, 1), ns = length(a[5], "spare", 1, 0),
                   n = length(a[10], "slot_map", 1, 0);
     return call((fn_t)address(a[0]), std::make_tuple(
-        c.address, array(a[2], "seq_len", kI32, {B}), array(a[3], "new_len", kI32, {B}), narrow(B, "B"), array(a[4], "block_table", kI32, {B, mb}),
-        narrow(mb, "max_blocks"), array(a[5], "spare", kI32, {ns}), narrow(ns, "spare"), array(a[6], "spare_used", kI32, {1}),
-        array(a[7], "spare_next", kI32, {1}), array(a[8], "end_len", kI32, {B}), array(a[9], "cu_new", kI32, {B + 1}),
-        array(a[10], "slot_map", kI64, {n}), array(a[11], "token_pos", kI32, {n}), array(a[12], "token_seq", kI32, {n}),
-        array(a[13], "full_block", kI32, {n}), narrow(n, "n_tokens"), array(a[14], "status", kI32, {2}), stream_of(a[15])));
+        c.address, c.array(a[2], "seq_len", kI32, {B}), c.array(a[3], "new_len", kI32, {B}), narrow(B, "B"), c.array(a[4], "block_table", kI32, {B, mb}),
+        narrow(mb, "max_blocks"), c.array(a[5], "spare", kI32, {ns}), narrow(ns, "spare"), c.array(a[6], "spare_used", kI32, {1}),
+        c.array(a[7], "spare_next", kI32, {1}), c.array(a[8], "end_len", kI32, {B}), c.array(a[9], "cu_new", kI32, {B + 1}),
+        c.array(a[10], "slot_map", kI64, {n}), c.array(a[11], "token_pos", kI32, {n}), c.array(a[12], "token_seq", kI32, {n}),
+        c.array(a[13], "full_block", kI32, {n}), narrow(n, "n_tokens"), c.array(a[14], "status", kI32, {2}), stream_of(a[15])));
 }
 
 // fn, ctx, layer, q, k, v, pos, sections (address or None), number of sections, rope_theta, slot_map, q_out, stream
@@ -188,10 +191,10 @@ int32_t rope_append(PyObject *const *a)
     void *sections = address(a[7]);
     if (sections && integer(a[8]) != axes) throw Refused{"sections for another number of axes"};
     int64_t qs, ks, vs;
-    void *q = rows(a[3], "q", c.type, n, c.hq, c.d, qs), *k = rows(a[4], "k", c.type, n, c.hkv, c.d, ks), *v = rows(a[5], "v", c.type, n, c.hkv, c.d, vs);
-    void *pos = one ? array(a[6], "pos", kI32, {n}) : array(a[6], "pos", kI32, {axes, n});
+    void *q = c.rows(a[3], "q", n, c.hq, qs), *k = c.rows(a[4], "k", n, c.hkv, ks), *v = c.rows(a[5], "v", n, c.hkv, vs);
+    void *pos = one ? c.array(a[6], "pos", kI32, {n}) : c.array(a[6], "pos", kI32, {axes, n});
     return call((fn_t)address(a[0]), std::make_tuple(c.address, narrow(integer(a[2]), "layer"), q, qs, k, ks, v, vs, pos, narrow(axes, "axes"), sections, real(a[9]),
-                                 array(a[10], "slot_map", kI64, {n}), narrow(n, "n_tokens"), array(a[11], "q_out", c.type, {n, c.hq, c.d}), stream_of(a[12])));
+                                 c.array(a[10], "slot_map", kI64, {n}), narrow(n, "n_tokens"), c.array(a[11], "q_out", c.type, {n, c.hq, c.d}), stream_of(a[12])));
 }
 
 // fn, ctx, l0, l1, entries, digests, stream
@@ -200,9 +203,9 @@ int32_t digest_blocks(PyObject *const *a)
     typedef int32_t (*fn_t)(void *, int32_t, int32_t, const void *, int32_t, void *, void *);
     const Ctx c(a[1]);
     int64_t n;
-    void *entries = any_shape(a[4], "entries", kI32, n);
+    void *entries = c.any_shape(a[4], "entries", kI32, n);
     return call((fn_t)address(a[0]), std::make_tuple(c.address, narrow(integer(a[2]), "l0"), narrow(integer(a[3]), "l1"), entries, narrow(n, "entries"),
-                                 array(a[5], "digests", at::kChar, {c.digest_bytes}), stream_of(a[6])));
+                                 c.array(a[5], "digests", at::kChar, {c.digest_bytes}), stream_of(a[6])));
 }
 
 // fn, ctx, layer, q, token_seq, token_pos, block_table, digests, n_sink, n_top, n_local, lists, workspace, stream
@@ -214,12 +217,12 @@ int32_t select_blocks(PyObject *const *a)
     const int64_t n = length(a[4], "token_seq", 1, 0), B = length(a[6], "block_table", 2, 0), mb = length(a[6], "block_table", 2, 1);
     const int32_t sink = narrow(integer(a[8]), "n_sink"), top = narrow(integer(a[9]), "n_top"), local = narrow(integer(a[10]), "n_local");
     int64_t bytes;
-    void *ws = any_shape(a[12], "workspace", at::kByte, bytes);
+    void *ws = c.any_shape(a[12], "workspace", at::kByte, bytes);
     return call((fn_t)address(a[0]), std::make_tuple(
-        c.address, narrow(integer(a[2]), "layer"), array(a[3], "q", c.type, {n, c.hq, c.d}), array(a[4], "token_seq", kI32, {n}),
-        array(a[5], "token_pos", kI32, {n}), narrow(n, "n_tokens"), array(a[6], "block_table", kI32, {B, mb}), narrow(B, "B"), narrow(mb, "max_blocks"),
-        array(a[7], "digests", at::kChar, {c.digest_bytes}), sink, top, local,
-        array(a[11], "lists", kI32, {n, c.hkv, (int64_t)sink + top + local}), ws, (size_t)bytes, stream_of(a[13])));
+        c.address, narrow(integer(a[2]), "layer"), c.array(a[3], "q", c.type, {n, c.hq, c.d}), c.array(a[4], "token_seq", kI32, {n}),
+        c.array(a[5], "token_pos", kI32, {n}), narrow(n, "n_tokens"), c.array(a[6], "block_table", kI32, {B, mb}), narrow(B, "B"), narrow(mb, "max_blocks"),
+        c.array(a[7], "digests", at::kChar, {c.digest_bytes}), sink, top, local,
+        c.array(a[11], "lists", kI32, {n, c.hkv, (int64_t)sink + top + local}), ws, (size_t)bytes, stream_of(a[13])));
 }
 
 // fn, ctx, layer, q, token_seq, token_pos, block_table, lists, out, sm_scale, workspace, stream
@@ -231,11 +234,11 @@ int32_t block_attn(PyObject *const *a)
     const int64_t n = length(a[4], "token_seq", 1, 0), B = length(a[6], "block_table", 2, 0), mb = length(a[6], "block_table", 2, 1),
                   nl = length(a[7], "lists", 3, 2);
     int64_t bytes;
-    void *ws = any_shape(a[10], "workspace", at::kByte, bytes);
+    void *ws = c.any_shape(a[10], "workspace", at::kByte, bytes);
     return call((fn_t)address(a[0]), std::make_tuple(
-        c.address, narrow(integer(a[2]), "layer"), array(a[3], "q", c.type, {n, c.hq, c.d}), array(a[4], "token_seq", kI32, {n}),
-        array(a[5], "token_pos", kI32, {n}), narrow(n, "n_tokens"), array(a[6], "block_table", kI32, {B, mb}), narrow(B, "B"), narrow(mb, "max_blocks"),
-        array(a[7], "lists", kI32, {n, c.hkv, nl}), narrow(nl, "lists"), array(a[8], "out", c.type, {n, c.hq, c.d}), (float)real(a[9]), ws,
+        c.address, narrow(integer(a[2]), "layer"), c.array(a[3], "q", c.type, {n, c.hq, c.d}), c.array(a[4], "token_seq", kI32, {n}),
+        c.array(a[5], "token_pos", kI32, {n}), narrow(n, "n_tokens"), c.array(a[6], "block_table", kI32, {B, mb}), narrow(B, "B"), narrow(mb, "max_blocks"),
+        c.array(a[7], "lists", kI32, {n, c.hkv, nl}), narrow(nl, "lists"), c.array(a[8], "out", c.type, {n, c.hq, c.d}), (float)real(a[9]), ws,
         (size_t)bytes, stream_of(a[11])));
 }
 

@@ -345,3 +345,18 @@ def test_encoded_queries_do_not_overwrite_rows_still_to_be_read(small_pool):
     torch.cuda.synchronize()
     assert torch.equal(wide, before)
     p.ctx.tc_rope_append(0, q[:1], kv[:1], kv[:1], SH.i32([1]), 1e4, slot[:1], out[:1])        # one row is read before it is written
+
+
+def test_tensors_of_another_device_are_refused(small_pool):
+    """As seen from a context of device 7: none of this machine's tensors are its own."""
+    from paper_2601_08743_amd import _py_step, binding as B
+    c, one = small_pool.ctx, SH.i32([1])
+    other = c._step[:6] + (7,)
+    assert c._step[6] == torch.cuda.current_device()
+    with pytest.raises(B.TcError, match="entries.* on device 7, got Int . 1 . on device 0"):
+        _py_step.digest_blocks(0, other, 0, 1, one, small_pool.digests(), None)
+    q, kv = small_pool.rows(1, 8, 1), small_pool.rows(1, 2, 2)
+    with pytest.raises(B.TcError, match="q: .* on device 7"):
+        _py_step.rope_append(0, other, 0, q, kv, kv, one, None, 0, 1e4, SH.i64([80]), q, None)
+    with pytest.raises(B.TcError, match="on device 7"):
+        _py_step.block_attn(0, other, 0, q, one, one, SH.i32([[1]]), SH.i32([[[0], [0]]]), q, 0.1, torch.zeros(16, dtype=torch.uint8, device="cuda"), None)

@@ -23,7 +23,7 @@ def test_step_tables_by_hand():
 
 
 def test_rotate_is_the_reencoding_of_the_stitch():
-    """With one axis the model is the checker's re-encoding; with several, each section is that of its own axis alone."""
+    """With one axis the model is the oracle's re-encoding; with several, each section is that of its own axis alone."""
     rng = np.random.default_rng(2)
     x, pos = rng.standard_normal((6, 2, 64)), rng.integers(0, 90000, size=(3, 6))
     np.testing.assert_allclose(S.rotate(x, pos[:1], [32], 1e4), oracle.reencode_keys(x, pos[0], 1e4), atol=1e-9)

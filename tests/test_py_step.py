@@ -10,7 +10,7 @@ from paper_2601_08743_amd import _py_step
 from paper_2601_08743_amd import binding as B
 
 _I, _P = ctypes.c_int32, ctypes.c_void_p
-CTX = (0x77, 8, 2, 64, 0, 1000)
+CTX = (0x77, 8, 2, 64, 0, 1000, 0)
 
 
 def _fail(*args):
@@ -46,7 +46,7 @@ def test_arguments_of_another_kind_are_errors_not_calls():
     with pytest.raises(TypeError):
         _py_step.digest_blocks(_addr(3), CTX, 0, 1, z, z)
     with pytest.raises(TypeError):
-        _py_step.digest_blocks(0, ("f", 8, 2, 64, 0, 1000), 0, 1, z, z, None)
+        _py_step.digest_blocks(0, ("f", 8, 2, 64, 0, 1000, 0), 0, 1, z, z, None)
     with pytest.raises(B.TcError, match="block_table: expected 2 dimensions"):
         _py_step.select_blocks(_addr(3), CTX, 0, z, z, z, z, z, 1, 2, 3, z, z, None)
     with pytest.raises(B.TcError, match="bad context"):
