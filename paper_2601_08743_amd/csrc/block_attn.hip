@@ -764,18 +764,16 @@ __device__ __forceinline__ void write_bf16x4(char *dst, f32x4 x)
 //
 // A work-group is (token, KV head, 16 rows, range of the list); its waves take the range's units in turn, keep their own
 // running maximum and sum, and are combined through LDS at the end.  No wave waits for another before that.
-struct ListUnit { int32_t j, entry; int valid; };
-
-// A row's partial outputs, maxima and sums of kParts waves, `apart` floats from wave to wave: four columns from d on of each, the maximum
-// and the sum at `ml`.
+// A row's partial outputs, maxima and sums of kParts waves: four columns of each, `apart` floats from wave to wave, and the two at `ml`,
+// `ml_apart` floats apart.
 template <int kParts>
-__device__ __forceinline__ RowSum fold_rows(const float *part, int apart, int ml, int d)
+__device__ __forceinline__ RowSum fold_rows(const float *part, int apart, const float *ml, int ml_apart)
 {
     RowSum x{-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
     float2 of[kParts];
 #pragma unroll
     for (int k = 0; k < kParts; ++k) {
-        of[k] = *(const float2 *)(part + k * apart + ml);
+        of[k] = *(const float2 *)(ml + k * ml_apart);
         x.M = fmaxf(x.M, of[k].x);
     }
 #pragma unroll
@@ -783,19 +781,17 @@ __device__ __forceinline__ RowSum fold_rows(const float *part, int apart, int ml
         // (no maximum: no keys - its sums are zeros - or only scores that are NaN, and so are they)
         const float wgt = of[k].x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(of[k].x - x.M);
         x.L += wgt * of[k].y;
-        x.acc += wgt * *(const f32x4 *)(part + k * apart + d);
+        x.acc += wgt * *(const f32x4 *)(part + k * apart);
     }
     return x;
 }
 
-// Block j of a list: its table entry and how many of its positions the token sees (0: none).
-__device__ __forceinline__ ListUnit list_unit(const Geom &g, const BlockAttnArgs &a, int32_t j, const int32_t *table, int pos)
+// Block j of a list: its table entry (-1: none), and how many of its positions the token sees (0: none).
+__device__ __forceinline__ int32_t listed_entry(const int32_t *table, int32_t j, int pos) { return j >= 0 && j <= pos >> 4 ? table[j] : -1; }
+__device__ __forceinline__ int listed_keys(const Geom &g, const BlockAttnArgs &a, int32_t j, int32_t entry, int pos)
 {
-    ListUnit u{j, -1, 0};
-    if (u.j >= 0 && u.j <= pos >> 4) u.entry = table[u.j];
-    const int bid = entry_bid(u.entry);
-    if (u.entry >= 0 && bid >= a.first_block && bid < g.n_blocks) u.valid = min(kBlockTokens - entry_pad(u.entry), pos - u.j * kBlockTokens + 1);
-    return u;
+    const int bid = entry_bid(entry);
+    return entry >= 0 && bid >= a.first_block && bid < g.n_blocks ? min(kBlockTokens - entry_pad(entry), pos - j * kBlockTokens + 1) : 0;
 }
 
 // bf16, heads of 128.  A unit is two blocks, 32 keys, against 16 query rows: S^T = K Q^T by 16x16x32 matrix instructions whose
@@ -808,20 +804,20 @@ __device__ __forceinline__ ListUnit list_unit(const Geom &g, const BlockAttnArgs
 // from there: loaded straight into the operands' registers, where neighbouring lanes are neighbouring rows of 256 bytes, keys take a
 // CU's address path 64 cycles a kilobyte instead of 16.  The next unit's keys are requested as soon as this one's are in
 // registers, and so the values.  (Values straight to registers, 32-byte rows, and twice the waves: slower for every list tried.)
-// Bound: 53 blocks for each of 4 items, 7.7 us, the chain of units; 49 for each of 128, 51 MB, 11.1 us = 4.6 TB/s, what a CU takes from
-// memory; 64 for each of 5.4 k items, 157 us, the L2's 2.8 GB = 18 TB/s, of which a fifth comes from further (all there: 105 us).
-constexpr int kBaRow = 132;                              // padded output row of the exchange (floats), maximum and sum behind it
+// Bound: 53 blocks for each of 4 items, 7.2 us, what one CU takes; 49 for each of 128, 51 MB, 10.9 us = 4.7 TB/s, likewise;
+// 64 for each of 5.4 k items, 155 us, the L2's 2.8 GB = 18 TB/s, of which a fifth comes from further (all there: 105 us).
 constexpr int kBaBlock = 4096;                           // one head's K (or V) in one block
 constexpr int kBaWaves = 4;
 constexpr int kBaWave = 4 * kBaBlock;                    // K of a unit: rows of 256 bytes, 16-byte chunk c of row r at c ^ r; V: two blocks verbatim
+constexpr int kBaChunk = 32 * kBaWaves;                  // units that a work-group looks up at a time, 32 a wave: lane 2k + b looks up block b of unit k
 
 constexpr float kBaRescale = 8.f;                        // weights grow to 2^8 before the reference moves
 
 template <bool kSplit>
 __global__ __launch_bounds__(64 * kBaWaves, 2) void block_attn_bf16_kernel(Geom g, BlockAttnArgs a)
 {
-    constexpr int kWaves = kBaWaves;
     extern __shared__ __attribute__((aligned(256))) char lds[];          // (the XOR addressing of the K rows needs them 256-byte aligned)
+    __shared__ float2 s_ml[kBaWaves][16];
     const int chunks = (int)a.chunks.by;
     const int item = a.splits(blockIdx.x), split = blockIdx.x - item * a.n_splits;
     const int head = a.chunks(item), n = a.heads(head), kvh = head - n * g.Hkv, row0 = (item - head * chunks) * 16;
@@ -830,10 +826,11 @@ __global__ __launch_bounds__(64 * kBaWaves, 2) void block_attn_bf16_kernel(Geom 
     const int32_t *list = a.lists + ((int64_t)n * g.Hkv + kvh) * a.n_list;
     const int n_units = (a.n_list + 1) >> 1;
     const int u0 = (int)((int64_t)n_units * split / a.n_splits), u1 = (int)((int64_t)n_units * (split + 1) / a.n_splits);
-    const int end = min(2 * u1, a.n_list);
-    // a wave's units 32 at a time: lane 2k + b looks up block b of unit k
-    auto listed = [&](int k0) { const int i = 2 * (k0 + kWaves * (lane >> 1)) + (lane & 1); return i < end ? list[i] : -1; };
-    int32_t j_next = listed(u0 + w);                     // (while the token's place is looked up)
+    auto listed = [&](int k0) {                          // this lane's block of the units from k0 on
+        const int i = 2 * (k0 + kBaWaves * (lane >> 1)) + (lane & 1);
+        return i < min(2 * u1, a.n_list) ? list[i] : -1;
+    };
+    int32_t j = listed(u0 + w);                          // (while the token's place is looked up)
     int seq, pos;
     if (!token_place(a.token_seq, a.token_pos, n, a.B, a.max_blocks, seq, pos)) return;
     const int32_t *table = a.block_table + (int64_t)seq * a.max_blocks;
@@ -842,6 +839,7 @@ __global__ __launch_bounds__(64 * kBaWaves, 2) void block_attn_bf16_kernel(Geom 
     const uint32_t lds_w = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + w * kBaWave;
     typedef const __attribute__((address_space(3))) bf16x8 *lds_frag;
 
+    int32_t entry = listed_entry(table, j, pos);
     bf16x8 qf[4];
     {
         const char *qr = a.q + ((int64_t)n * g.Hq + kvh * g.G + row0 + min(r16, rows - 1)) * 256 + q4 * 16;
@@ -863,109 +861,114 @@ __global__ __launch_bounds__(64 * kBaWaves, 2) void block_attn_bf16_kernel(Geom 
     const uint32_t kr = (uint32_t)(r16 & 7), kb = lds_w + (r16 >> 3) * kBaBlock + kr * 256 + ((q4 ^ kr) << 4);
     const uint32_t vb = lds_w + 2 * kBaBlock + (q4 >> 1) * kBaBlock + r16 * 32 + (q4 & 1) * 16;
 
-    for (int k0 = u0 + w; k0 < u1; k0 += kWaves * 32) {
-        const ListUnit mine = list_unit(g, a, j_next, table, pos);
-        j_next = listed(k0 + kWaves * 32);
-        const uint64_t some = __ballot(mine.valid > 0);
-        if (some == 0) continue;
-        const int n_mine = (65 - __builtin_clzll(some)) >> 1;        // up to the last unit with a key
-        asm volatile("" : "+v"(qf[0]), "+v"(qf[1]), "+v"(qf[2]), "+v"(qf[3]));      // (in registers: nothing but the counted loads is outstanding from here on)
-        auto sources = [&](int k, const char *(&src)[2]) {
-            const int v0 = __builtin_amdgcn_readlane(mine.valid, 2 * k), v1 = __builtin_amdgcn_readlane(mine.valid, 2 * k + 1);
-            const int b0 = entry_bid(__builtin_amdgcn_readlane(mine.entry, 2 * k)), b1 = entry_bid(__builtin_amdgcn_readlane(mine.entry, 2 * k + 1));
-            // (what is loaded in an empty block's place is masked)
-            src[0] = pool + (int64_t)(v0 > 0 ? b0 : v1 > 0 ? b1 : a.first_block) * g.block_bytes;
-            src[1] = pool + (int64_t)(v1 > 0 ? b1 : v0 > 0 ? b0 : a.first_block) * g.block_bytes;
-        };
-        auto issue_k = [&](const char *const (&src)[2]) {
-            load4_to_lds(lds_w, src[0], k_off);
-            load4_to_lds(lds_w + kBaBlock, src[1], k_off);
-        };
-        auto issue_v = [&](const char *const (&src)[2]) {
-            load4_to_lds(lds_w + 2 * kBaBlock, src[0] + v_half, v_off);
-            load4_to_lds(lds_w + 3 * kBaBlock, src[1] + v_half, v_off);
-        };
-        const char *src[2];
-        sources(0, src);
-        issue_k(src);
-        issue_v(src);
-        for (int k = 0; k < n_mine; ++k) {
-            const bool more = k + 1 < n_mine;
-            wait_loads<8>();                             // K is there, V may be on its way
-            bf16x8 kf[8];
+    int keys;
+    const char *src[2];
+    auto sources = [&](int k) {
+        const int v0 = __builtin_amdgcn_readlane(keys, 2 * k), v1 = __builtin_amdgcn_readlane(keys, 2 * k + 1);
+        const int b0 = entry_bid(__builtin_amdgcn_readlane(entry, 2 * k)), b1 = entry_bid(__builtin_amdgcn_readlane(entry, 2 * k + 1));
+        // (what is loaded in an empty block's place is masked)
+        src[0] = pool + (int64_t)(v0 > 0 ? b0 : v1 > 0 ? b1 : a.first_block) * g.block_bytes;
+        src[1] = pool + (int64_t)(v1 > 0 ? b1 : v0 > 0 ? b0 : a.first_block) * g.block_bytes;
+    };
+    auto issue_k = [&]() {
+        load4_to_lds(lds_w, src[0], k_off);
+        load4_to_lds(lds_w + kBaBlock, src[1], k_off);
+    };
+    auto issue_v = [&]() {
+        load4_to_lds(lds_w + 2 * kBaBlock, src[0] + v_half, v_off);
+        load4_to_lds(lds_w + 3 * kBaBlock, src[1] + v_half, v_off);
+    };
+    // Unit k, whose keys and values were requested before; those of the next one, where there are more, as the areas become free.
+    auto unit = [&](int k, bool more) __attribute__((always_inline)) {
+        const int valid0 = __builtin_amdgcn_readlane(keys, 2 * k), valid1 = __builtin_amdgcn_readlane(keys, 2 * k + 1);
+        wait_loads<8>();                                 // K is there, V may be on its way
+        bf16x8 kf[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) kf[i] = *(lds_frag)(uintptr_t)(((kb ^ ((i & 3) << 6)) ^ ((i >> 2) << 7)) + (i >> 2) * 2048);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // K area read out
-            if (more) {
-                sources(k + 1, src);
-                issue_k(src);
-            }
-            f32x4 s[2];
+        for (int i = 0; i < 8; ++i) kf[i] = *(lds_frag)(uintptr_t)(((kb ^ ((i & 3) << 6)) ^ ((i >> 2) << 7)) + (i >> 2) * 2048);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // K area read out
+        if (more) {
+            sources(k + 1);
+            issue_k();
+        }
+        f32x4 s[2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int h = 0; h < 2; ++h) {
+            s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int ks = 0; ks < 4; ++ks) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[4 * h + ks], qf[ks], s[h], 0, 0, 0);
-            }
-            if (more) wait_loads<8>();
-            else wait_loads<0>();
-            bf16x8 vf[8];
+            for (int ks = 0; ks < 4; ++ks) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[4 * h + ks], qf[ks], s[h], 0, 0, 0);
+        }
+        if (more) wait_loads<8>();
+        else wait_loads<0>();
+        bf16x8 vf[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) vf[i] = *(lds_frag)(uintptr_t)(vb + i * 512);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // V area read out
-            if (more) issue_v(src);
-            const int valid0 = __builtin_amdgcn_readlane(mine.valid, 2 * k), valid1 = __builtin_amdgcn_readlane(mine.valid, 2 * k + 1);
-            if (valid0 < kBlockTokens || valid1 < kBlockTokens) {
-                const int seen = (q4 < 2 ? valid0 : valid1) - 4 * (q4 & 1);      // of this lane's tokens 0..3 and 8..11
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const bool sees = 8 * h + e < seen;
-                        s[h][e] = sees ? s[h][e] : -INFINITY;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) vf[i][4 * h + e] = sees ? vf[i][4 * h + e] : (__bf16)0.f;
-                    }
-            }
-            float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-            const float mxs = max_over<16>(mx) * a.scale_log2;
-            if (__any(mxs > m_run + kBaRescale)) {       // also taken while m_run is still -inf
-                const float m_new = fmaxf(m_run, mxs);
-                const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
-                l_lane *= alpha;
-#pragma unroll
-                for (int db = 0; db < 8; ++db)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[db][e] *= alpha;
-                m_run = m_new;
-            }
-            const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
-            bf16x8 pf;
+        for (int i = 0; i < 8; ++i) vf[i] = *(lds_frag)(uintptr_t)(vb + i * 512);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // V area read out
+        if (more) issue_v();
+        if (valid0 < kBlockTokens || valid1 < kBlockTokens) {
+            const int seen = (q4 < 2 ? valid0 : valid1) - 4 * (q4 & 1);      // of this lane's tokens 0..3 and 8..11
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(s[h][e], a.scale_log2, neg_m));
-                    l_lane += p;
-                    pf[4 * h + e] = (__bf16)p;
-                }
+                    const bool sees = 8 * h + e < seen;
+                    s[h][e] = sees ? s[h][e] : -INFINITY;
 #pragma unroll
-            for (int db = 0; db < 8; ++db) o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[db], pf, o[db], 0, 0, 0);
+                    for (int i = 0; i < 8; ++i) vf[i][4 * h + e] = sees ? vf[i][4 * h + e] : (__bf16)0.f;
+                }
         }
+        float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+        const float mxs = max_over<16>(mx) * a.scale_log2;
+        if (__any(mxs > m_run + kBaRescale)) {   // also taken while m_run is still -inf
+            const float m_new = fmaxf(m_run, mxs);
+            const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
+            l_lane *= alpha;
+#pragma unroll
+            for (int db = 0; db < 8; ++db)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[db][e] *= alpha;
+            m_run = m_new;
+        }
+        const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
+        bf16x8 pf;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(s[h][e], a.scale_log2, neg_m));
+                l_lane += p;
+                pf[4 * h + e] = (__bf16)p;
+            }
+#pragma unroll
+        for (int db = 0; db < 8; ++db) o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[db], pf, o[db], 0, 0, 0);
+    };
+    for (int k0 = u0 + w; k0 < u1; k0 += kBaChunk) {
+        keys = listed_keys(g, a, j, entry, pos);
+        const uint64_t some = __ballot(keys > 0);
+        const int units = some ? (65 - __builtin_clzll(some)) >> 1 : 0;      // up to the last one with a key
+        asm volatile("" : "+v"(qf[0]), "+v"(qf[1]), "+v"(qf[2]), "+v"(qf[3]));      // (in registers: nothing but the counted loads is outstanding from here on)
+        if (units > 0) {
+            sources(0);
+            issue_k();
+            issue_v();
+            for (int k = 0; k + 1 < units; ++k) unit(k, true);
+            unit(units - 1, false);
+        }
+        if (k0 + kBaChunk < u1) entry = listed_entry(table, j = listed(k0 + kBaChunk), pos);
     }
 
-    // the waves' (output, maximum, sum) rows, combined by 32 threads a row, four columns each
+    // the waves' (output, maximum, sum) rows, combined by 32 threads a row, four columns each: chunk c of row r at c ^ r of the V area
     const float l_row = sum_over<16>(l_lane);
     if (r16 < rows) {
-        float *mine = (float *)(lds + w * kBaWave) + r16 * kBaRow;
+        char *mine = lds + w * kBaWave + 2 * kBaBlock + r16 * 512;
 #pragma unroll
-        for (int db = 0; db < 8; ++db) *(f32x4 *)(mine + 16 * db + 4 * q4) = o[db];
-        if (q4 == 0) *(float2 *)(mine + 128) = make_float2(m_run, l_row);
+        for (int db = 0; db < 8; ++db) *(f32x4 *)(mine + (((4 * db + q4) ^ r16) << 4)) = o[db];
+        if (q4 == 0) s_ml[w][r16] = make_float2(m_run, l_row);
     }
     __syncthreads();
-    const int d = 4 * (tid & 31);
-    for (int row = tid >> 5; row < rows; row += 2 * kWaves) {
-        const RowSum x = fold_rows<kWaves>((const float *)lds + row * kBaRow, kBaWave / (int)sizeof(float), 128, d);
+    const int c = tid & 31, d = 4 * c;
+    for (int row = tid >> 5; row < rows; row += 2 * kBaWaves) {
+        const RowSum x = fold_rows<kBaWaves>((const float *)(lds + 2 * kBaBlock + row * 512 + ((c ^ row) << 4)), kBaWave / (int)sizeof(float),
+                                             (const float *)&s_ml[0][row], 16 * 2);
         const int64_t out_row = (int64_t)n * g.Hq + kvh * g.G + row0 + row;
         if (kSplit) {
             *(f32x4 *)(a.part_o + (out_row * a.n_splits + split) * 128 + d) = x.acc;
@@ -1007,12 +1010,13 @@ __global__ __launch_bounds__(256, 2) void block_attn_f32_kernel(Geom g, BlockAtt
         l_run[r] = 0.f;
     }
     for (int k0 = u0 + w; k0 < u1; k0 += kWaves * 64) {
-        const ListUnit mine = list_unit(g, a, k0 + kWaves * lane < u1 ? list[k0 + kWaves * lane] : -1, table, pos);
+        const int32_t j = k0 + kWaves * lane < u1 ? list[k0 + kWaves * lane] : -1, entry = listed_entry(table, j, pos);
+        const int keys = listed_keys(g, a, j, entry, pos);
         const int n_mine = min(64, (u1 - k0 + kWaves - 1) / kWaves);
         for (int k = 0; k < n_mine; ++k) {
-            const int valid = __builtin_amdgcn_readlane(mine.valid, k);
+            const int valid = __builtin_amdgcn_readlane(keys, k);
             if (valid <= 0) continue;
-            const char *p = pool + (int64_t)entry_bid(__builtin_amdgcn_readlane(mine.entry, k)) * g.block_bytes;
+            const char *p = pool + (int64_t)entry_bid(__builtin_amdgcn_readlane(entry, k)) * g.block_bytes;
             f32x4 kf[kSteps], vf[kSteps];
 #pragma unroll
             for (int t = 0; t < kSteps; ++t) kf[t] = *(const f32x4 *)(p + (t * kGroups + grp) * (kD * 4));
@@ -1068,7 +1072,7 @@ __global__ __launch_bounds__(256, 2) void block_attn_f32_kernel(Geom g, BlockAtt
     constexpr int kThreadsRow = kD / 4;
     for (int row = tid / kThreadsRow; row < rows; row += 64 * kWaves / kThreadsRow) {
         const int d = 4 * (tid % kThreadsRow);
-        const RowSum x = fold_rows<kWaves>(s_part + row * kRow, kRows * kRow, kD, d);
+        const RowSum x = fold_rows<kWaves>(s_part + row * kRow + d, kRows * kRow, s_part + row * kRow + kD, kRows * kRow);
         const int64_t out_row = (int64_t)n * g.Hq + kvh * g.G + row0 + row;
         if (kSplit) {
             *(f32x4 *)(a.part_o + (out_row * a.n_splits + split) * kD + d) = x.acc;
@@ -1118,7 +1122,7 @@ __global__ __launch_bounds__(256) void block_merge_kernel(Geom g, BlockAttnArgs 
 }
 
 // Ranges of a list.  Four waves to a work-group: two of them share a CU where items fill the chip, and their starts and ends overlap
-// (5.4 k bf16 items of 64 blocks: 157 us; with eight waves 205), and for few items eight waves are no faster.
+// (5.4 k bf16 items of 64 blocks: 155 us; with eight waves 205), and for few items eight waves are no faster.
 //   bf16: a work-group reads a list at what a CU takes from memory, some 80 GB/s, so ranges of eight units, two a wave, for work-groups of
 //   their own pay for the launch that combines them (4 us with the gap) where lists are long and few: a pass of scores, list and attention
 //   takes, in ranges and in one, for 8 lists of 80 blocks 13.6 and 15.6 us, of 160 14.7 and 21.2; for 32 of 80 15.2 and 16.8, of 128
