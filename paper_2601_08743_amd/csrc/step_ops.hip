@@ -176,7 +176,7 @@ hipError_t launch_step_tables(const StepTables &s, const Launch &L)
 // A work-group a token: its (cos, sin) table in LDS, then a thread for every pair of 16-byte chunks.  The values of a bf16 block are
 // stored transposed, two bytes of a token in each row of 32; tokens that go to the same block therefore share its KV heads
 // out among their work-groups, each of which takes those heads' rows of all of them and writes whole rows.  Bound: memory, for many tokens
-// (2048, 32 / 8 heads, 50 MB: 11.0 us = 4.6 TB/s; 21.8 with two-byte stores); slot, position and row one after the other for few
+// (2048, 32 / 8 heads, 50 MB: 10.8 us = 4.7 TB/s; 21.8 with two-byte stores); slot, position and row one after the other for few
 // (32 tokens 4.5 us).
 struct Run { int first, len; };                          // the step's tokens of one block
 
@@ -203,6 +203,24 @@ __global__ __launch_bounds__(256) void rope_append_kernel(Geom g, RopeAppend a)
     if (slot < 0 || blk < g.first_seq || blk >= g.n_blocks) return;     // a padded row, or no block of a sequence
     const int t = (int)(slot & 15);
     const int half_d = g.D >> 1, cph = g.head_bytes >> 4, half_c = cph >> 1, half_log = __builtin_ctz(half_c);   // (chunks of a head: 16 or 32)
+    const int rot_units = (g.Hq + g.Hkv) * half_c;
+    auto source = [&](int u) {                           // of a pair of chunks
+        const int h = u >> half_log, cc = u & (half_c - 1);
+        return (h < g.Hq ? a.q + n * a.q_stride + (int64_t)h * g.head_bytes : a.k + n * a.k_stride + (int64_t)(h - g.Hq) * g.head_bytes) + (cc << 4);
+    };
+    auto values = [&](int r) { return *(const uint4 *)(a.v + n * a.v_stride + (int64_t)(r >> (half_log + 1)) * g.head_bytes + ((r & (cph - 1)) << 4)); };
+    const Run run = run_of(a, n, slot, tid & 63);
+    const int t_run = t - (n - run.first);               // the run's first position; 0: the block begins here, and is zero behind the run
+    const bool by_run = kBf16 && t_run == 0;
+    const int v_units = by_run ? 0 : g.Hkv * cph;
+    // a thread's first chunks, requested while the turns are computed
+    uint4 x, y, v;
+    if (tid < rot_units) {
+        const char *src = source(tid);
+        x = *(const uint4 *)src;
+        y = *(const uint4 *)(src + (half_c << 4));
+    }
+    if (tid < v_units) v = values(tid);
     if (tid < half_d) {
         int axis = 0;
         while (tid >= a.section_end[axis]) ++axis;
@@ -217,36 +235,33 @@ __global__ __launch_bounds__(256) void rope_append_kernel(Geom g, RopeAppend a)
         }
         cs[tid] = make_float2(c, sn);
     }
-    const Run run = run_of(a, n, slot, tid & 63);
-    const int t_run = t - (n - run.first);               // the run's first position; 0: the block begins here, and is zero behind the run
     char *kd = g.pool + (int64_t)a.layer * g.layer_stride + blk * g.block_bytes;
     char *vd = kd + (g.block_bytes >> 1);
     constexpr int kElems = kBf16 ? 8 : 4;
-    const bool by_run = kBf16 && t_run == 0;
     __syncthreads();
-    const int rot_units = (g.Hq + g.Hkv) * half_c, units = rot_units + (by_run ? 0 : g.Hkv * cph);
-    for (int u = tid; u < units; u += 256) {
-        if (u < rot_units) {
-            const int h = u >> half_log, cc = u & (half_c - 1);
-            const bool is_q = h < g.Hq;
-            const char *src = (is_q ? a.q + n * a.q_stride + (int64_t)h * g.head_bytes : a.k + n * a.k_stride + (int64_t)(h - g.Hq) * g.head_bytes) + (cc << 4);
-            char *dst = (is_q ? a.q_out + ((int64_t)n * g.Hq + h) * g.head_bytes : kd + (int64_t)((h - g.Hq) * kBlockTokens + t) * g.head_bytes) + (cc << 4);
-            uint4 x = *(const uint4 *)src, y = *(const uint4 *)(src + (half_c << 4));
-            turn_chunk<kBf16>(x, y, cs + cc * kElems);
-            *(uint4 *)dst = x;
-            *(uint4 *)(dst + (half_c << 4)) = y;
+    for (int u = tid; u < rot_units; u += 256) {
+        const int h = u >> half_log, cc = u & (half_c - 1);
+        char *dst = (h < g.Hq ? a.q_out + ((int64_t)n * g.Hq + h) * g.head_bytes : kd + (int64_t)((h - g.Hq) * kBlockTokens + t) * g.head_bytes) + (cc << 4);
+        if (u != tid) {
+            const char *src = source(u);
+            x = *(const uint4 *)src;
+            y = *(const uint4 *)(src + (half_c << 4));
+        }
+        turn_chunk<kBf16>(x, y, cs + cc * kElems);
+        *(uint4 *)dst = x;
+        *(uint4 *)(dst + (half_c << 4)) = y;
+    }
+    for (int r = tid; r < v_units; r += 256) {
+        if (r != tid) v = values(r);
+        const int h = r >> (half_log + 1), cc = r & (cph - 1);
+        if (!kBf16) {
+            *(uint4 *)(vd + (int64_t)(h * kBlockTokens + t) * g.head_bytes + (cc << 4)) = v;
         } else {
-            const int r = u - rot_units, h = r >> (half_log + 1), cc = r & (cph - 1);
-            const uint4 v = *(const uint4 *)(a.v + n * a.v_stride + (int64_t)h * g.head_bytes + (cc << 4));
-            if (!kBf16) {
-                *(uint4 *)(vd + (int64_t)(h * kBlockTokens + t) * g.head_bytes + (cc << 4)) = v;
-            } else {
-                const unsigned e[4] = {v.x, v.y, v.z, v.w};
-                unsigned short *v16 = (unsigned short *)vd;
+            const unsigned e[4] = {v.x, v.y, v.z, v.w};
+            unsigned short *v16 = (unsigned short *)vd;
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    v16[((int64_t)(h * g.D + cc * 8 + k) << 4) + vperm(t)] = (unsigned short)(e[k >> 1] >> ((k & 1) * 16));
-            }
+            for (int k = 0; k < 8; ++k)
+                v16[((int64_t)(h * g.D + cc * 8 + k) << 4) + vperm(t)] = (unsigned short)(e[k >> 1] >> ((k & 1) * 16));
         }
     }
     const uint4 zero = make_uint4(0, 0, 0, 0);
@@ -271,11 +286,13 @@ __global__ __launch_bounds__(256) void rope_append_kernel(Geom g, RopeAppend a)
         }
     }
     if (t == 0 && run.len < kBlockTokens) {
-        const int rows = kBlockTokens - run.len, cpr = g.row_bytes >> 4;
-        for (int c = tid; c < rows * cpr; c += 256) {
-            const int tt = run.len + c / cpr, w = c % cpr, h = w / cph, cc = w - h * cph;
-            *(uint4 *)(kd + (int64_t)(h * kBlockTokens + tt) * g.head_bytes + (cc << 4)) = zero;
-            if (!kBf16) *(uint4 *)(vd + (int64_t)(h * kBlockTokens + tt) * g.head_bytes + (cc << 4)) = zero;
+        const int chunks = (kBlockTokens - run.len) * cph;               // behind one another in a head's rows
+        for (int h = 0; h < g.Hkv; ++h) {
+            const int64_t at = (int64_t)(h * kBlockTokens + run.len) * g.head_bytes;
+            for (int c = tid; c < chunks; c += 256) {
+                *(uint4 *)(kd + at + (c << 4)) = zero;
+                if (!kBf16) *(uint4 *)(vd + at + (c << 4)) = zero;
+            }
         }
     }
 }
