@@ -58,7 +58,7 @@ template <int kD>
 struct QueryRows {                                       // 16 rows as a wave holds them
     static constexpr int kSteps = 2 * kD / 64;           // matrix instructions along the 2D products
     i32x4 a[kSteps];
-    float scale[4];                                      // of rows 4 q4 + e, whose products stand in this lane: 2^f, -1 for a row that takes no part
+    float scale[4];                                      // of rows 4 q4 + e, whose products stand in this lane: 2^f, NaN for a row that takes no part
 };
 
 // 16 query rows made ready in LDS by 256 threads, 16 a row: [max(qi, 0) | min(qi, 0)], 16-byte chunk c of row r at c ^ r.  (Made by every
@@ -94,7 +94,7 @@ struct QueryTile {
         const bool finite = __float_as_uint(size) < 0x7f800000u;
         const int f = finite ? step_exponent(size) : 0;
         const float by = step_pow2(-f);
-        if (c == 0) scale[r] = finite && counts ? step_pow2(f) : -1.f;
+        if (c == 0) scale[r] = finite && counts ? step_pow2(f) : __builtin_nanf("");
         uint32_t plus[kOwn / 4], minus[kOwn / 4];
 #pragma unroll
         for (int j = 0; j < kOwn / 4; ++j) {
@@ -169,7 +169,8 @@ struct BoundsTile {
     }
 };
 
-// Products of this lane's four rows of each tile with its block, each by its row's power of two (the tiles' chains side by side).
+// Products of this lane's four rows of each tile with its block, each by its row's power of two (the tiles' chains side by side); NaN of
+// a row that takes no part, which no maximum of two numbers picks.
 template <int kD, int kTiles>
 __device__ __forceinline__ void tile_products(f32x4 (&p)[kTiles], const QueryRows<kD> (&q)[kTiles], const i32x4 (&b)[QueryRows<kD>::kSteps])
 {
@@ -183,7 +184,7 @@ __device__ __forceinline__ void tile_products(f32x4 (&p)[kTiles], const QueryRow
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) p[t][e] = q[t].scale[e] < 0.f ? -INFINITY : (float)acc[t][e] * q[t].scale[e];
+        for (int e = 0; e < 4; ++e) p[t][e] = (float)acc[t][e] * q[t].scale[e];
 }
 __device__ __forceinline__ float column_max(f32x4 p)     // over the 16 rows, in every quarter
 {
@@ -274,12 +275,12 @@ __global__ __launch_bounds__(256) void score_token_kernel(Geom g, SelectArgs a)
 }
 
 // 4 (16 / G) neighbouring tokens, four tiles of query rows: suffixes, whose tokens read the same digests.  Tokens of another request
-// follow with a pass of their own.  (681 tokens of eight requests, 8 KV heads, 380 to 849 blocks: 22.7 us.)  The products of rows 4 q4 + e of tile t stand in quarter q4 of a wave, so these sixteen
+// follow with a pass of their own.  (681 tokens of eight requests, 8 KV heads, 380 to 849 blocks: 21.8 us.)  The products of rows 4 q4 + e of tile t stand in quarter q4 of a wave, so these sixteen
 // are the heads of 16 / G whole tokens, one after the other, and a token's largest is found in registers.
 constexpr int kTiles = 4;
 
 template <bool kBf16, int kD>
-__global__ __launch_bounds__(256) void score_group_kernel(Geom g, SelectArgs a)
+__global__ __launch_bounds__(256, 2) void score_group_kernel(Geom g, SelectArgs a)
 {
     typedef BoundsTile<kD> Tile;
     __shared__ __attribute__((aligned(256))) char s_tile[4][2][Tile::kBytes];
@@ -680,7 +681,7 @@ __global__ __launch_bounds__(1024) void score_select_kernel(Geom g, SelectArgs a
             if (k + 2 < rounds) load(k + 2);
             f32x4 p[1];
             tile_products<kD>(p, q, b);
-            float m = column_max(p[0]);
+            float m = fmaxf(column_max(p[0]), -INFINITY);      // (no row takes part)
             const int i = 256 * k + 16 * w + r16;
             if (q4 == 0 && i < cand) {
                 if (row0 > 0) m = fmaxf(m, s_prod[i]);   // (of this wave's own earlier rows)

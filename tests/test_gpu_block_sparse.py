@@ -194,6 +194,28 @@ def test_lists_over_tables_of_some_thousand_blocks(hq, hkv, d, dtype, max_blocks
     pool.close()
 
 
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(8, 2, 128, "bf16"), (40, 2, 128, "bf16"), (34, 2, 64, "f32")])
+@pytest.mark.parametrize("max_blocks", [900, 1900])
+def test_lists_of_queries_that_are_not_finite(hq, hkv, d, dtype, max_blocks):
+    """One head, the first or the last ones of a group, or all of it, for one launch and for two."""
+    pool = SH.Pool(hq, hkv, d, dtype, 60)
+    pool.fill(8)
+    table = np.random.default_rng(max_blocks).integers(0, 60, size=(6, max_blocks))
+    digests = _digested(pool, np.arange(60))
+    G = hq // hkv
+    q = pool.rows(6, hq, 3)
+    q[0, :, 5] = float("nan")
+    q[1, 0, 0] = float("inf")
+    q[2, G:, 7] = float("-inf")
+    q[3, :G - 1, 1] = float("nan")
+    q[4, 1:G, 1] = float("nan")
+    seq, pos = list(range(6)), [16 * max_blocks - 1] * 6
+    for sink, top, local in ((1, 30, 2), (0, 300, 1)):
+        got = _lists(pool, q, seq, pos, table, digests, sink, top, local)
+        np.testing.assert_array_equal(got, _want_lists(pool, q, seq, pos, table, digests, sink, top, local))
+    pool.close()
+
+
 @pytest.mark.parametrize("max_blocks", [257, 1024, 1025])
 def test_lists_of_many_tokens_over_long_tables(max_blocks):
     """More than a thousand lists, from every number of candidates; few different blocks, so scores are tied."""
