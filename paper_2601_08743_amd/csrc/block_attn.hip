@@ -750,14 +750,11 @@ hipError_t launch_select(const Geom &g, SelectArgs a, const Launch &L)
 }
 
 // ------------------------------------------------------------------------------------ attention
-__device__ __forceinline__ void write_bf16x4(char *dst, f32x4 x)
+__device__ __forceinline__ uint32_t bf16_pair(float x, float y)
 {
-    uint32_t r[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-        r[k] = (uint32_t)__builtin_bit_cast(unsigned short, (__bf16)x[2 * k]) | ((uint32_t)__builtin_bit_cast(unsigned short, (__bf16)x[2 * k + 1]) << 16);
-    *(uint2 *)dst = make_uint2(r[0], r[1]);
+    return (uint32_t)__builtin_bit_cast(unsigned short, (__bf16)x) | ((uint32_t)__builtin_bit_cast(unsigned short, (__bf16)y) << 16);
 }
+__device__ __forceinline__ void write_bf16x4(char *dst, f32x4 x) { *(uint2 *)dst = make_uint2(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])); }
 
 // out = softmax(sm_scale q . k) v over the keys of the listed blocks at positions up to the token's own that hold a token;
 // zeros where there are none.  A token and KV head have G rows that share a list, so as in the decode kernel the work is
@@ -766,11 +763,12 @@ __device__ __forceinline__ void write_bf16x4(char *dst, f32x4 x)
 // A work-group is (token, KV head, 16 rows, range of the list); its waves take the range's units in turn, keep their own
 // running maximum and sum, and are combined through LDS at the end.  No wave waits for another before that.
 // A row's partial outputs, maxima and sums of kParts waves: four columns of each, `apart` floats from wave to wave, and the two at `ml`,
-// `ml_apart` floats apart.
+// `ml_apart` floats apart.  `rest`: a wave's sums that belong to those `rest` floats before them, where they are finite (0: none).
 template <int kParts>
-__device__ __forceinline__ RowSum fold_rows(const float *part, int apart, const float *ml, int ml_apart)
+__device__ __forceinline__ RowSum fold_rows(const float *part, int apart, const float *ml, int ml_apart, int rest)
 {
     RowSum x{-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
+    f32x4 rests = {0.f, 0.f, 0.f, 0.f};
     float2 of[kParts];
 #pragma unroll
     for (int k = 0; k < kParts; ++k) {
@@ -783,6 +781,11 @@ __device__ __forceinline__ RowSum fold_rows(const float *part, int apart, const 
         const float wgt = of[k].x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(of[k].x - x.M);
         x.L += wgt * of[k].y;
         x.acc += wgt * *(const f32x4 *)(part + k * apart);
+        if (rest != 0) rests += wgt * *(const f32x4 *)(part + rest + k * apart);
+    }
+    if (rest != 0) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x.acc[e] += __builtin_isfinite(rests[e]) ? rests[e] : 0.f;
     }
     return x;
 }
@@ -798,8 +801,11 @@ __device__ __forceinline__ int listed_keys(const Geom &g, const BlockAttnArgs &a
 // bf16, heads of 128.  A unit is two blocks, 32 keys, against 16 query rows: S^T = K Q^T by 16x16x32 matrix instructions whose
 // 16 keys are tokens 0..7 of both blocks, then 8..15, so that a lane's eight scores (quarter q4 of the wave: block q4 / 2,
 // half q4 % 2) belong to the eight tokens whose values stand in one 16-byte piece of the pool's V rows, and O^T += V^T P^T
-// takes both as they are.  Weights are rounded to bf16 for that product (as in every attention kernel here; their sum is of
-// the fp32 ones).  Values at positions that the token does not see are replaced by zeros, whatever stands there.
+// takes both as they are.  A weight goes into that product as a sum of two bf16 numbers, itself rounded and what that leaves out, so
+// that 16 bits of it count and the output's own rounding is the one that shows.  Up to eight rows have their rests in the columns that
+// would be copies (kRest: rows behind the eighth), more rows in instructions of their own.  The rests' sums are kept apart and left out where they
+// are no finite number: an infinite value times a rest of zero, or of the other sign, is not what the formula has.  Values at positions that the
+// token does not see are replaced by zeros, whatever stands there.
 //
 // A unit's 16 KB come by direct loads into the wave's own piece of LDS, a kilobyte of neighbouring bytes each, and the operands
 // from there: loaded straight into the operands' registers, where neighbouring lanes are neighbouring rows of 256 bytes, keys take a
@@ -814,7 +820,7 @@ constexpr int kBaChunk = 32 * kBaWaves;                  // units that a work-gr
 
 constexpr float kBaRescale = 8.f;                        // weights grow to 2^8 before the reference moves
 
-template <bool kSplit>
+template <bool kSplit, bool kRest>
 __global__ __launch_bounds__(64 * kBaWaves, 2) void block_attn_bf16_kernel(Geom g, BlockAttnArgs a)
 {
     extern __shared__ __attribute__((aligned(256))) char lds[];          // (the XOR addressing of the K rows needs them 256-byte aligned)
@@ -843,13 +849,15 @@ __global__ __launch_bounds__(64 * kBaWaves, 2) void block_attn_bf16_kernel(Geom 
     int32_t entry = listed_entry(table, j, pos);
     bf16x8 qf[4];
     {
-        const char *qr = a.q + ((int64_t)n * g.Hq + kvh * g.G + row0 + min(r16, rows - 1)) * 256 + q4 * 16;
+        const char *qr = a.q + ((int64_t)n * g.Hq + kvh * g.G + row0 + min(kRest ? r16 & 7 : r16, rows - 1)) * 256 + q4 * 16;
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) qf[ks] = *(const bf16x8 *)(qr + ks * 64);
     }
-    f32x4 o[8];
+    f32x4 o[8], o_rest[8];                               // by the weights in bf16, and by what they leave out (kRest: both in o)
 #pragma unroll
-    for (int db = 0; db < 8; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int db = 0; db < 8; ++db) o[db] = o_rest[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const bool rests = !kRest || r16 >= 8;               // what of a weight in bf16, in the lower and upper half of a register, is taken from it
+    const uint32_t low_half = rests ? 0x01000c0cu : 0x0c0c0c0cu, high_half = rests ? 0xffff0000u : 0u;
     float m_run = -INFINITY, l_lane = 0.f;
 
     uint32_t k_off[4], v_off[4];
@@ -926,21 +934,33 @@ __global__ __launch_bounds__(64 * kBaWaves, 2) void block_attn_bf16_kernel(Geom 
 #pragma unroll
             for (int db = 0; db < 8; ++db)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[db][e] *= alpha;
+                for (int e = 0; e < 4; ++e) {
+                    o[db][e] *= alpha;
+                    if (!kRest) o_rest[db][e] *= alpha;
+                }
             m_run = m_new;
         }
         const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
-        bf16x8 pf;
+        bf16x8 pf, rest;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(s[h][e], a.scale_log2, neg_m));
-                l_lane += p;
-                pf[4 * h + e] = (__bf16)p;
+            for (int e = 0; e < 4; e += 2) {
+                const float p0 = __builtin_amdgcn_exp2f(fmaf(s[h][e], a.scale_log2, neg_m)), p1 = __builtin_amdgcn_exp2f(fmaf(s[h][e + 1], a.scale_log2, neg_m));
+                l_lane += p0;
+                l_lane += p1;
+                const uint32_t both = bf16_pair(p0, p1);
+                // (kRest: the lanes of the first eight columns subtract nothing)
+                const float r0 = p0 - __uint_as_float(__builtin_amdgcn_perm(0u, both, low_half)), r1 = p1 - __uint_as_float(both & high_half);
+                const uint32_t left = bf16_pair(r0, r1);
+                ((uint32_t *)&pf)[2 * h + e / 2] = kRest ? left : both;
+                ((uint32_t *)&rest)[2 * h + e / 2] = left;
             }
 #pragma unroll
-        for (int db = 0; db < 8; ++db) o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[db], pf, o[db], 0, 0, 0);
+        for (int db = 0; db < 8; ++db) {
+            o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[db], pf, o[db], 0, 0, 0);
+            if (!kRest) o_rest[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[db], rest, o_rest[db], 0, 0, 0);
+        }
     };
     for (int k0 = u0 + w; k0 < u1; k0 += kBaChunk) {
         keys = listed_keys(g, a, j, entry, pos);
@@ -959,7 +979,13 @@ __global__ __launch_bounds__(64 * kBaWaves, 2) void block_attn_bf16_kernel(Geom 
 
     // the waves' (output, maximum, sum) rows, combined by 32 threads a row, four columns each: chunk c of row r at c ^ r of the V area
     const float l_row = sum_over<16>(l_lane);
-    if (r16 < rows) {
+    if (!kRest) {
+#pragma unroll
+        for (int db = 0; db < 8; ++db)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[db][e] += __builtin_isfinite(o_rest[db][e]) ? o_rest[db][e] : 0.f;
+    }
+    if ((kRest ? r16 & 7 : r16) < rows) {                // (kRest: the rests as rows eight further on)
         char *mine = lds + w * kBaWave + 2 * kBaBlock + r16 * 512;
 #pragma unroll
         for (int db = 0; db < 8; ++db) *(f32x4 *)(mine + (((4 * db + q4) ^ r16) << 4)) = o[db];
@@ -968,8 +994,9 @@ __global__ __launch_bounds__(64 * kBaWaves, 2) void block_attn_bf16_kernel(Geom 
     __syncthreads();
     const int c = tid & 31, d = 4 * c;
     for (int row = tid >> 5; row < rows; row += 2 * kBaWaves) {
-        const RowSum x = fold_rows<kBaWaves>((const float *)(lds + 2 * kBaBlock + row * 512 + ((c ^ row) << 4)), kBaWave / (int)sizeof(float),
-                                             (const float *)&s_ml[0][row], 16 * 2);
+        const float *part = (const float *)(lds + 2 * kBaBlock + row * 512 + ((c ^ row) << 4));
+        const int to_rest = kRest ? 8 * 128 + ((c & 8) ? -32 : 32) : 0;          // row + 8's chunk c stands at c ^ (row + 8)
+        const RowSum x = fold_rows<kBaWaves>(part, kBaWave / (int)sizeof(float), (const float *)&s_ml[0][row], 16 * 2, to_rest);
         const int64_t out_row = (int64_t)n * g.Hq + kvh * g.G + row0 + row;
         if (kSplit) {
             *(f32x4 *)(a.part_o + (out_row * a.n_splits + split) * 128 + d) = x.acc;
@@ -1073,7 +1100,7 @@ __global__ __launch_bounds__(256, 2) void block_attn_f32_kernel(Geom g, BlockAtt
     constexpr int kThreadsRow = kD / 4;
     for (int row = tid / kThreadsRow; row < rows; row += 64 * kWaves / kThreadsRow) {
         const int d = 4 * (tid % kThreadsRow);
-        const RowSum x = fold_rows<kWaves>(s_part + row * kRow + d, kRows * kRow, s_part + row * kRow + kD, kRows * kRow);
+        const RowSum x = fold_rows<kWaves>(s_part + row * kRow + d, kRows * kRow, s_part + row * kRow + kD, kRows * kRow, 0);
         const int64_t out_row = (int64_t)n * g.Hq + kvh * g.G + row0 + row;
         if (kSplit) {
             *(f32x4 *)(a.part_o + (out_row * a.n_splits + split) * kD + d) = x.acc;
@@ -1167,15 +1194,15 @@ static hipError_t launch_attn_f32(const Geom &g, const BlockAttnArgs &a, unsigne
     return hipGetLastError();
 }
 
-template <bool kSplit>
+template <bool kSplit, bool kRest>
 static hipError_t launch_attn_bf16(const Geom &g, const BlockAttnArgs &a, unsigned grid, const Launch &L)
 {
     static PerDeviceOnce configured;
     const hipError_t e = configured.run([] {
-        return hipFuncSetAttribute((const void *)block_attn_bf16_kernel<kSplit>, hipFuncAttributeMaxDynamicSharedMemorySize, kBaWaves * kBaWave);
+        return hipFuncSetAttribute((const void *)block_attn_bf16_kernel<kSplit, kRest>, hipFuncAttributeMaxDynamicSharedMemorySize, kBaWaves * kBaWave);
     });
     if (e != hipSuccess) return e;
-    TC_LAUNCH_N(block_attn_bf16_kernel<kSplit>, grid, 64 * kBaWaves, kBaWaves * kBaWave, L, g, a);
+    TC_LAUNCH_N((block_attn_bf16_kernel<kSplit, kRest>), grid, 64 * kBaWaves, kBaWaves * kBaWave, L, g, a);
     return hipGetLastError();
 }
 
@@ -1190,7 +1217,8 @@ hipError_t launch_block_attn(const Geom &g, BlockAttnArgs a, const Launch &L)
     a.heads = FastDiv((uint32_t)g.Hkv);
     const bool split = a.n_splits > 1;
     const unsigned n = (unsigned)grid;
-    if (g.esize == 2) return split ? launch_attn_bf16<true>(g, a, n, L) : launch_attn_bf16<false>(g, a, n, L);
+    if (g.esize == 2 && g.G <= 8) return split ? launch_attn_bf16<true, true>(g, a, n, L) : launch_attn_bf16<false, true>(g, a, n, L);
+    if (g.esize == 2) return split ? launch_attn_bf16<true, false>(g, a, n, L) : launch_attn_bf16<false, false>(g, a, n, L);
     if (g.D == 64) return split ? launch_attn_f32<64, true>(g, a, n, L) : launch_attn_f32<64, false>(g, a, n, L);
     return split ? launch_attn_f32<128, true>(g, a, n, L) : launch_attn_f32<128, false>(g, a, n, L);
 }
