@@ -171,7 +171,9 @@ hipError_t launch_step_tables(const StepTables &s, const Launch &L)
 // Queries and keys turned by position - pair (j, j + D/2) of every head by pos * theta^(-2j/D), the position being that of the
 // axis whose section j falls into - and keys and values written to their slots, in one pass over the rows.  As in the
 // re-encoding stitch the turn is a fraction of a revolution taken in fp64, sine and cosine and the rotation are fp32 and the
-// result is rounded once.
+// result is rounded once.  The fraction is the one of the smaller size, -1/2 to 1/2, so that turns just below a whole one keep their
+// bits; what its fp32 form leaves out, up to 2 pi 2^-26, is more than the rounding of a sine, and goes into fp32 results by the
+// derivatives.
 //
 // A work-group a token: its (cos, sin) table in LDS, then a thread for every pair of 16-byte chunks.  The values of a bf16 block are
 // stored transposed, two bytes of a token in each row of 32; tokens that go to the same block therefore share its KV heads
@@ -225,13 +227,18 @@ __global__ __launch_bounds__(256) void rope_append_kernel(Geom g, RopeAppend a)
         int axis = 0;
         while (tid >= a.section_end[axis]) ++axis;
         const double turns = (double)a.pos[(int64_t)axis * a.n_tokens + n] * (a.rev_coarse[tid >> 3] * a.rev_fine[tid & 7]);
-        const float frac = (float)(turns - floor(turns));
+        const double part = turns - rint(turns);
+        const float frac = (float)part;
         float sn, c;
         if (kBf16) {
             sn = __builtin_amdgcn_sinf(frac);
             c = __builtin_amdgcn_cosf(frac);
         } else {
-            sincospif(2.0f * frac, &sn, &c);
+            const float left = 6.28318531f * (float)(part - (double)frac);
+            float sn0, c0;
+            sincospif(2.0f * frac, &sn0, &c0);
+            sn = fmaf(left, c0, sn0);
+            c = fmaf(-left, sn0, c0);
         }
         cs[tid] = make_float2(c, sn);
     }
