@@ -315,8 +315,9 @@ hipError_t launch_rope_append(const Geom &g, const RopeAppend &a, const Launch &
 // ------------------------------------------------------------------------------------ digests
 // Bounds of a block's keys, channel by channel, in 8 bits with one power of two for all: hi = max over the block's tokens, lo =
 // min; e the smallest integer, -126 at least, with max(|hi|, |lo|) <= 127 * 2^e; stored are ceil(hi / 2^e) and
-// floor(lo / 2^e), so that they stay bounds, and e (127 where some key is not finite).  Dividing by a power of two is exact:
-// the bytes follow from the keys alone, whatever computes them.
+// floor(lo / 2^e), so that they stay bounds, and e (127 where some key is not finite).  Dividing by a power of two is exact, but for
+// quotients too small for fp32, and those are bounded by 1 as any up to 1 are: the bytes follow from the keys alone, whatever computes
+// them.
 //
 // One read of the keys: a wave takes one block of one KV head, 16 rows that stand behind one another, and holds 16 bytes of each
 // fourth (or second) row in a lane.  Maximum and minimum are taken on the bits, made to order like integers, in which
@@ -411,7 +412,7 @@ __global__ __launch_bounds__(256) void digest_kernel(Geom g, DigestArgs a)
     uint32_t bytes = 0;
 #pragma unroll
     for (int q = 0; q < kOwn; ++q) {
-        const float y = ceilf(bound[q] * by);
+        const float y = fmaxf(ceilf(bound[q] * by), (int)__float_as_uint(bound[q]) > 0 ? 1.f : -INFINITY);
         bytes |= ((uint32_t)(finite ? (int)(is_lo ? -y : y) : 0) & 0xffu) << (8 * q);
     }
     const int64_t to = ((int64_t)layer * g.Hkv + h) * g.n_blocks + bid;
