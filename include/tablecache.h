@@ -373,14 +373,16 @@ tc_status tc_table_entries(tc_ctx *ctx, const int32_t *block_table, int64_t n, i
  * gets blocks for positions [seq_len[b], seq_len[b] + new_len[b]) behind the ceil(seq_len[b] / 16) it has: the entries
  * spare[spare_used[0]], spare[spare_used[0] + 1], .. in order, requests in order.  Tokens are numbered request by
  * request, in position order.
- *   spare [n_spare]         ids of sequence blocks to take; one that is none becomes -1 in the row, its tokens get no slot
+ *   spare [n_spare]         ids of sequence blocks to take; one that is none becomes -1 in the row
  *   spare_used, spare_next  [1] entries taken before, and behind, this step (may be the same address)
  *   end_len [B]             seq_len + new_len (may be seq_len itself, which then advances)
  *   cu_new [B + 1]          first token of each request, and the number of tokens
  *   slot_map, token_pos, token_seq, full_block [n_tokens]
  *                           16 * block + position % 16; position; request; the block's id where the token takes its last slot,
- *                           else -1.  Rows behind the step's tokens are -1 in all four.
- *   status [2]              0 (or an error of this list), and the number of blocks taken:
+ *                           else -1.  Rows behind the step's tokens are -1 in all four, and so are those of tokens whose block (a spare
+ *                           id, or the entry under a request's partial last block) is no sequence block: no call makes anything of them.
+ *   status [2]              0, 1 where there are such tokens (the rest of the step is made), or an error of this list, and the number
+ *                           of blocks taken:
  *                           TC_ERR_OOM_POOL   the spare entries do not suffice (status[1]: how many blocks the step takes)
  *                           TC_ERR_INVALID    a length is negative or ends beyond max_blocks * 16, more than n_tokens new
  *                                             tokens, or spare_used is no place of spare

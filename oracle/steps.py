@@ -26,7 +26,7 @@ def step_tables(seq_len, new_len, table, spare, used: int, n_tokens: int, first_
     need = [(l + s + 15) // 16 - (l + 15) // 16 for l, s in zip(seq_len, new_len)]
     if sum(need) > len(spare) - used:
         return refused(-3, sum(need))
-    at, n = used, 0
+    at, n, whole = used, 0, True
     for b in range(B):
         have = (seq_len[b] + 15) // 16
         for j in range(have, have + need[b]):
@@ -35,14 +35,16 @@ def step_tables(seq_len, new_len, table, spare, used: int, n_tokens: int, first_
         for p in range(seq_len[b], seq_len[b] + new_len[b]):
             block = int(table[b, p // 16])
             block = block & ((1 << 27) - 1) if block >= 0 else -1
-            rows["token_seq"][n], rows["token_pos"][n] = b, p
-            if block >= 0:
+            if first_seq <= block < n_blocks:
+                rows["token_seq"][n], rows["token_pos"][n] = b, p
                 rows["slot_map"][n] = 16 * block + p % 16
                 if p % 16 == 15:
                     rows["full_block"][n] = block
+            else:
+                whole = False
             n += 1
     return dict(rows, table=table, spare_next=at, end_len=np.array(seq_len) + np.array(new_len),
-                cu_new=np.concatenate([[0], np.cumsum(new_len)]), status=np.array([0, sum(need)]))
+                cu_new=np.concatenate([[0], np.cumsum(new_len)]), status=np.array([0 if whole else 1, sum(need)]))
 
 
 def rotate(x: np.ndarray, pos: np.ndarray, sections: Sequence[int], theta: float) -> np.ndarray:

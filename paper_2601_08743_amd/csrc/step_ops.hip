@@ -18,6 +18,10 @@ namespace tc {
 // and writes its part (300 requests, 5.0 k tokens: 6.2 us so, 10 in one work-group).  Where the results are to stand in place of
 // the inputs that the other work-groups still read, the sums are a launch of their own and the second takes the lengths from its
 // results.
+//
+// A token whose block is none - a spare id, or an entry under a partial last block, that names no sequence block - is no token to any call
+// behind this one, and the status says that there are such.  One work-group knows when it has written its rows; of several one has no rows
+// and looks at the blocks instead, while the others write.
 template <int kThreads, bool kScan, bool kFill>
 __global__ __launch_bounds__(kThreads) void step_tables_kernel(StepTables s)
 {
@@ -27,7 +31,8 @@ __global__ __launch_bounds__(kThreads) void step_tables_kernel(StepTables s)
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, B = s.B;
     int32_t *cu = lds, *held = lds + B + 1, *first = held + B;
     // (a fill launch of its own finds the step's end lengths, and the cursor behind the step's blocks)
-    const bool refused = !kScan && s.status[0] != 0;
+    const bool refused = !kScan && s.status[0] < 0;
+    const bool alone = kScan && kFill && gridDim.x == 1, sums = kScan && blockIdx.x == gridDim.x - 1;    // (the work-group that writes the sums)
     const int32_t used = kScan ? s.spare_used[0] : s.spare_next[0] - (refused ? 0 : s.status[1]);
     uint64_t n_new = 0;                                 // of the requests so far; a request counts n_tokens at most, a round of them 2^30
     uint32_t n_blocks = 0;
@@ -71,25 +76,49 @@ __global__ __launch_bounds__(kThreads) void step_tables_kernel(StepTables s)
     int32_t code = bad || n_new > (uint64_t)s.n_tokens ? -1 : 0;
     if (code == 0 && (int32_t)n_blocks > s.n_spare - used) code = -3;
     const int32_t total = code == 0 ? (int32_t)n_new : 0;
-    if (kScan && blockIdx.x == 0) {
+    auto is_block = [&](int32_t id) { return id >= s.first_seq && id < s.n_blocks; };
+    bool none = false;                                  // a token's block is none
+    if (sums) {
         for (int b = tid; b < B; b += kThreads) {       // (a thread's own requests)
+            const int32_t fresh = code == 0 ? s.new_len[b] : 0, len = held[b];
             s.cu_new[b] = code == 0 ? cu[b] : 0;
-            s.end_len[b] = held[b] + (code == 0 ? s.new_len[b] : 0);
+            s.end_len[b] = len + fresh;
+            if (!alone && fresh > 0 && (len & 15) != 0) {
+                const int32_t id = s.block_table[(int64_t)b * s.max_blocks + (len >> 4)];
+                none |= id < 0 || !is_block(entry_bid(id));
+            }
         }
+        if (!alone && code == 0)
+            for (int i = tid; i < (int)n_blocks; i += kThreads) none |= !is_block(s.spare[used + i]);
         if (tid == 0) {
             s.cu_new[B] = total;
             s.spare_next[0] = used + (code == 0 ? (int32_t)n_blocks : 0);
-            s.status[0] = code;
             s.status[1] = code == -1 ? 0 : (int32_t)n_blocks;
         }
+    }
+    auto report = [&]() {
+        const bool any = __any(none);
+        __syncthreads();                                // (s_bad was read)
+        if (lane == 0) s_bad[0][w] = any;
+        __syncthreads();
+        if (tid != 0) return;
+        int32_t is = code;
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) is = s_bad[0][k] != 0 && is == 0 ? 1 : is;
+        s.status[0] = is;
+    };
+    if (sums && !alone) {                               // (of several work-groups the last has no tokens)
+        report();
+        return;
     }
     if (!kFill) return;
     if (tid == 0) cu[B] = INT32_MAX;
     __syncthreads();
+    const int groups = kScan && !alone ? gridDim.x - 1 : gridDim.x;
     constexpr int kSide = 4;
     int top = 1;
     while (2 * top < B) top *= 2;
-    for (int n0 = blockIdx.x * (kSide * kThreads) + tid; n0 < s.n_tokens; n0 += gridDim.x * (kSide * kThreads)) {
+    for (int n0 = blockIdx.x * (kSide * kThreads) + tid; n0 < s.n_tokens; n0 += groups * (kSide * kThreads)) {
         int lo[kSide] = {0, 0, 0, 0};                   // the last request whose first token is not behind the token
         for (int step = top; step > 0; step >>= 1)
 #pragma unroll
@@ -119,24 +148,22 @@ __global__ __launch_bounds__(kThreads) void step_tables_kernel(StepTables s)
             int64_t slot = -1;
             int32_t full = -1;
             if (n < total) {
-                int32_t block;
-                if (fresh[k]) {
-                    block = id[k] < s.first_seq || id[k] >= s.n_blocks ? -1 : id[k];
-                    if ((pos[k] & 15) == 0) *entry[k] = block;
-                } else {
-                    block = id[k] < 0 ? -1 : entry_bid(id[k]);
-                }
-                if (block >= 0) {
+                const int32_t block = id[k] < 0 || fresh[k] ? id[k] : entry_bid(id[k]);
+                const bool is = is_block(block);
+                if (fresh[k] && (pos[k] & 15) == 0) *entry[k] = is ? block : -1;
+                if (is) {
                     slot = (int64_t)block * kBlockTokens + (pos[k] & 15);
                     if ((pos[k] & 15) == 15) full = block;
                 }
+                none |= !is;
             }
             s.slot_map[n] = slot;
-            s.token_pos[n] = pos[k];
-            s.token_seq[n] = n < total ? lo[k] : -1;
+            s.token_pos[n] = slot < 0 ? -1 : pos[k];
+            s.token_seq[n] = slot < 0 ? -1 : lo[k];
             s.full_block[n] = full;
         }
     }
+    if (alone) report();
 }
 
 constexpr int kTablesOneWg = 2048;
@@ -150,7 +177,7 @@ static hipError_t launch_tables(const StepTables &s, const Launch &L)
                                    (3 * kStepMaxSeqs + 1) * (int)sizeof(int32_t));
     });
     if (e != hipSuccess) return e;
-    const int grid = !kFill || s.n_tokens <= kTablesOneWg ? 1 : (s.n_tokens + 4 * kThreads - 1) / (4 * kThreads);
+    const int fill = (s.n_tokens + 4 * kThreads - 1) / (4 * kThreads), grid = !kFill || s.n_tokens <= kTablesOneWg ? 1 : fill + (kScan ? 1 : 0);
     TC_LAUNCH_N((step_tables_kernel<kThreads, kScan, kFill>), grid, kThreads, (3 * (size_t)s.B + 1) * sizeof(int32_t), L, s);
     return hipGetLastError();
 }
