@@ -82,7 +82,7 @@ struct tc_ctx {
     std::vector<hipEvent_t> read_ring;     // events recorded after stitch kernels
     std::vector<uint32_t> read_gen;        // how often each ring entry has been recorded
     int32_t read_next = 0;
-    hipEvent_t raw_ev = nullptr;           // block-format slots: the raw staging area was last used up to here,
+    hipEvent_t raw_ev = nullptr;           // block-format slots: the raw staging area was last used, or readers waited for, up to here,
     hipStream_t raw_stream = nullptr;      // on this stream
     bool raw_pending = false;
     static constexpr int kStepStreams = 32;
@@ -161,6 +161,21 @@ hipError_t wait_for_reader(tc_ctx *ctx, Slot &s, hipStream_t stream)
     }
     s.read_ev = -1;
     return hipStreamWaitEvent(stream, ctx->read_ring[ev], 0);
+}
+
+// Block-format slots: loads take turns in the staging area, each behind the last one's use of it.
+hipError_t wait_for_staging(tc_ctx *ctx, hipStream_t stream)
+{
+    return ctx->raw_pending && ctx->raw_stream != stream ? hipStreamWaitEvent(stream, ctx->raw_ev, 0) : hipSuccess;
+}
+
+hipError_t staging_used(tc_ctx *ctx, hipStream_t stream)
+{
+    const hipError_t e = hipEventRecord(ctx->raw_ev, stream);
+    if (e != hipSuccess) return e;
+    ctx->raw_stream = stream;
+    ctx->raw_pending = true;
+    return hipSuccess;
 }
 
 // Run `launch` on `stream`; with profiling on, give it two events that receive the dispatch's
@@ -539,7 +554,6 @@ tc_status tc_load_async(tc_ctx *ctx, const int32_t *table_ids, int32_t n, int32_
                         if (ev < 0) return fail(ctx, TC_ERR_HIP, "load: hipEventRecord failed");
                         TC_HIP(ctx, hipStreamWaitEvent(stream, ctx->read_ring[ev], 0));
                     }
-                // (a later load on another stream comes behind this one: they take turns in the staging area)
                 ctx->n_step_readers = 0;
             }
             if (s.reader_pending) {     // attention launches read the previous occupant in place: wait for
@@ -552,6 +566,14 @@ tc_status tc_load_async(tc_ctx *ctx, const int32_t *table_ids, int32_t n, int32_
                         if (o.reader_pending && o.reader_stream == s.reader_stream) o.reader_pending = false;
                 }
                 s.reader_pending = false;
+            }
+            // What this stream waits for here, no later load waits for again, in this slot or another.  Those on other streams come
+            // behind it all the same: by the slot's `ready` event, and with block-format slots, whose readers are those of any
+            // slot, by that of the staging area - which the copies below record, where there are any.
+            touched.insert(t.slot);
+            if (ctx->cfg.slot_layout == TC_SLOTS_BLOCKS && l0 == l1) {
+                TC_HIP(ctx, wait_for_staging(ctx, stream));
+                TC_HIP(ctx, staging_used(ctx, stream));
             }
         }
         ctx->trace.push_back(id); ctx->trace.push_back(hit ? 1 : 0); ctx->trace.push_back(evicted);
@@ -566,8 +588,10 @@ tc_status tc_load_async(tc_ctx *ctx, const int32_t *table_ids, int32_t n, int32_
             const bool blocks = ctx->cfg.slot_layout == TC_SLOTS_BLOCKS;
             // block-format slots: the rows land in the staging area (one for all tables; copies and
             // the kernel that lays them out into the slot's blocks are ordered by the stream)
-            if (blocks && ctx->raw_pending && ctx->raw_stream != stream)
-                TC_HIP(ctx, hipStreamWaitEvent(stream, ctx->raw_ev, 0));
+            if (blocks) TC_HIP(ctx, wait_for_staging(ctx, stream));
+            Slot &s = ctx->slots[t.slot];
+            if (hit && s.ready_pending && s.ready_stream != stream)    // the load that took the slot, and what it waited for
+                TC_HIP(ctx, hipStreamWaitEvent(stream, s.ready, 0));
             char *dst = (blocks ? g.tab_base : g.tab_base + (int64_t)t.slot * g.slot_bytes) + (size_t)l * width;
             touched.insert(t.slot);
             TC_HIP(ctx, hipMemcpyAsync(dst, t.host_k + (size_t)l * width, width * (e - l), hipMemcpyHostToDevice, stream));
@@ -576,9 +600,7 @@ tc_status tc_load_async(tc_ctx *ctx, const int32_t *table_ids, int32_t n, int32_
             if (blocks) {
                 TC_HIP(ctx, launch_format(g, g.tab_base, g.slot_bytes >> 1, t.n_tokens, t.slot * ctx->slot_blocks, l, e,
                                           Launch{stream, nullptr, nullptr}));
-                TC_HIP(ctx, hipEventRecord(ctx->raw_ev, stream));
-                ctx->raw_stream = stream;
-                ctx->raw_pending = true;
+                TC_HIP(ctx, staging_used(ctx, stream));
             }
             for (int x = l; x < e; ++x) t.layer_loaded[x] = 1;
             t.n_loaded += e - l;
