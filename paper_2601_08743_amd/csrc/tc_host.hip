@@ -17,6 +17,7 @@
 #include <map>
 #include <memory>
 #include <mutex>
+#include <new>
 #include <set>
 #include <string>
 #include <unordered_map>
@@ -85,9 +86,8 @@ struct tc_ctx {
     hipEvent_t raw_ev = nullptr;           // block-format slots: the raw staging area was last used, or readers waited for, up to here,
     hipStream_t raw_stream = nullptr;      // on this stream
     bool raw_pending = false;
-    static constexpr int kStepStreams = 32;
-    hipStream_t step_readers[kStepStreams] = {};   // block-format slots: streams with token-step calls, which may read any slot,
-    int32_t n_step_readers = 0;                    // since the last load that waited for them (kStepStreams + 1: more than fit)
+    std::vector<hipStream_t> step_readers; // block-format slots: streams with token-step calls, which may read any slot, since the
+                                           // last load that waited for them
     Plan plan;
     int32_t *h_stage = nullptr; size_t h_stage_ints = 0;    // pinned
     StageHalves stage;
@@ -545,17 +545,13 @@ tc_status tc_load_async(tc_ctx *ctx, const int32_t *table_ids, int32_t n, int32_
             TC_HIP(ctx, wait_for_reader(ctx, s, stream));   // a stitch may still be reading the previous occupant
             if (s.ready_pending && s.ready_stream != stream)   // earlier copies into this slot on another stream
                 TC_HIP(ctx, hipStreamWaitEvent(stream, s.ready, 0));
-            if (ctx->n_step_readers > 0) {      // token-step calls: everything enqueued so far on the streams they run on
-                if (ctx->n_step_readers > tc_ctx::kStepStreams) TC_HIP(ctx, hipDeviceSynchronize());
-                else
-                    for (int32_t r = 0; r < ctx->n_step_readers; ++r) {
-                        if (ctx->step_readers[r] == stream) continue;
-                        const int32_t ev = record_read(ctx, ctx->step_readers[r]);
-                        if (ev < 0) return fail(ctx, TC_ERR_HIP, "load: hipEventRecord failed");
-                        TC_HIP(ctx, hipStreamWaitEvent(stream, ctx->read_ring[ev], 0));
-                    }
-                ctx->n_step_readers = 0;
+            for (hipStream_t reader : ctx->step_readers) {     // token-step calls: everything enqueued so far on the streams they run on
+                if (reader == stream) continue;
+                const int32_t ev = record_read(ctx, reader);
+                if (ev < 0) return fail(ctx, TC_ERR_HIP, "load: hipEventRecord failed");
+                TC_HIP(ctx, hipStreamWaitEvent(stream, ctx->read_ring[ev], 0));
             }
+            ctx->step_readers.clear();
             if (s.reader_pending) {     // attention launches read the previous occupant in place: wait for
                                         // everything enqueued so far on the stream they run on
                 if (s.reader_stream != stream) {
@@ -1160,15 +1156,17 @@ static tc_status layer_check(tc_ctx *ctx, const char *what, int32_t layer)
     return TC_OK;
 }
 
-// A launch that may read table slots in place (which, only the device knows): the next load that takes a slot waits for it.
-static void slots_read(tc_ctx *ctx, hipStream_t stream)
+// Ahead of launches that may read table slots in place (which, only the device knows): the next load that takes a slot waits for them.
+static tc_status slots_read(tc_ctx *ctx, const char *what, hipStream_t stream)
 {
-    if (ctx->cfg.slot_layout != TC_SLOTS_BLOCKS) return;
-    const int32_t n = ctx->n_step_readers;
-    for (int32_t k = 0; k < std::min(n, tc_ctx::kStepStreams); ++k)
-        if (ctx->step_readers[k] == stream) return;
-    if (n < tc_ctx::kStepStreams) ctx->step_readers[n] = stream;
-    ctx->n_step_readers = std::min(n + 1, tc_ctx::kStepStreams + 1);
+    std::vector<hipStream_t> &readers = ctx->step_readers;
+    if (ctx->cfg.slot_layout != TC_SLOTS_BLOCKS || std::find(readers.begin(), readers.end(), stream) != readers.end()) return TC_OK;
+    try {
+        readers.push_back(stream);
+    } catch (const std::bad_alloc &) {
+        return fail(ctx, TC_ERR_CAPACITY, "%s: no host memory for another stream", what);
+    }
+    return TC_OK;
 }
 
 static bool misaligned(const void *p, size_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
@@ -1286,11 +1284,12 @@ tc_status tc_digest_blocks(tc_ctx *ctx, int32_t l0, int32_t l1, const int32_t *e
     a.exps_at = (int64_t)ctx->cfg.n_layers * ctx->cfg.n_kv_heads * ctx->cfg.n_pool_blocks * 2 * ctx->cfg.head_dim;
     a.first_block = (int32_t)first_pool_block(ctx->cfg);
     const int32_t at_once = (int32_t)std::max<int64_t>(4 * kStepMaxGroups / ctx->cfg.n_kv_heads, 1);
+    const tc_status noted = slots_read(ctx, "digest", stream);
+    if (noted != TC_OK) return noted;
     for (int32_t left = n; left > 0; left -= a.n, a.entries += a.n) {
         a.n = std::min(left, at_once);
         TC_HIP(ctx, launch_digest(ctx->geom, a, l1, Launch{stream, nullptr, nullptr}));
     }
-    slots_read(ctx, stream);
     return TC_OK;
 }
 
@@ -1360,6 +1359,8 @@ tc_status tc_block_attn(tc_ctx *ctx, int32_t layer, const void *q, const int32_t
     a.part_o = (float *)workspace;
     if (need > 0) a.part_ml = a.part_o + (size_t)n_tokens * g.Hq * splits * g.D;
     const int32_t at_once = (int32_t)std::max<int64_t>(kStepMaxGroups / ((int64_t)block_attn_groups(g.Hq, g.Hkv, g.esize) * splits), 1);
+    st = slots_read(ctx, "block attn", stream);
+    if (st != TC_OK) return st;
     for (int32_t left = n_tokens; left > 0; left -= a.n_tokens) {        // (more than one launch only of lists in one range)
         a.n_tokens = std::min(left, at_once);
         TC_HIP(ctx, timed_launch(ctx, 2, stream, [&](const Launch &ln) { return launch_block_attn(ctx->geom, a, ln); }));
@@ -1368,7 +1369,6 @@ tc_status tc_block_attn(tc_ctx *ctx, int32_t layer, const void *q, const int32_t
         a.lists += (int64_t)a.n_tokens * g.Hkv * n_list; a.token_seq += a.n_tokens; a.token_pos += a.n_tokens;
     }
     if (a.n_splits > 1) TC_HIP(ctx, timed_launch(ctx, 3, stream, [&](const Launch &ln) { return launch_block_merge(ctx->geom, a, ln); }));
-    slots_read(ctx, stream);
     return TC_OK;
 }
 

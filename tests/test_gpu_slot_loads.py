@@ -137,3 +137,28 @@ def test_layers_of_a_table_on_two_streams_are_all_there_for_a_stitch():
         want, _ = H.oracle_sequences(wl, dw.tables_np, layer, 0)
         np.testing.assert_array_equal(got, want)
     dw.close()
+
+
+def test_steps_on_many_streams_do_not_make_a_load_wait_on_the_host():
+    """Steps on the default stream and 32 others, one of them behind long work: the load that takes a slot returns while that runs, and
+    its rows come behind all of them."""
+    busy = Busy()
+    wl, dw = _resident(8, 4, True)
+    bt, pl = dw.ctx.tc_stitch_alias(wl.table_ids, wl.cu_tables, wl.suffix_len, 40 + 4 * dw.slot_blocks)
+    streams = [torch.cuda.default_stream()] + [torch.cuda.Stream() for _ in range(32)]
+    assert len({s.cuda_stream for s in streams}) == 33
+    steps = [_step_arrays(dw, wl, bt, pl) for _ in streams]
+    torch.cuda.synchronize()
+    busy.on(streams[7])
+    done = []
+    for st, s in zip(streams, steps):
+        _attend(dw, s, st)
+        done.append(torch.cuda.Event())
+        done[-1].record(st)
+    dw.ctx.tc_load_async([4], 0, wl.cfg.n_layers, streams[20])
+    assert not done[7].query()
+    streams[20].synchronize()
+    assert all(e.query() for e in done)
+    for s in steps[1:]:
+        assert torch.equal(s["out"], steps[0]["out"])
+    dw.close()
