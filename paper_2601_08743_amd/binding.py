@@ -29,9 +29,25 @@ if not os.path.exists(LIB_PATH):
 
 _lib = ctypes.CDLL(LIB_PATH)
 try:
-    from . import _py_call, _py_step
+    from . import _py_call
 except ImportError as e:
-    raise ImportError("_py_call.so or _py_step.so is not built (%s). Run `python -m paper_2601_08743_amd.build`." % e) from e
+    raise ImportError("_py_call.so is not built (%s). Run `python -m paper_2601_08743_amd.build`." % e) from e
+
+
+class _NotBuilt:
+    """In the place of a module: calls that need it raise, the others do not."""
+
+    def __init__(self, name: str, cause: ImportError):
+        self._said, self._cause = "%s.so is not built (%s). Run `python -m paper_2601_08743_amd.build`." % (name, cause), cause
+
+    def __getattr__(self, name):
+        raise ImportError(self._said) from self._cause
+
+
+try:
+    from . import _py_step              # (built against torch's own headers, which not every torch brings: only the token steps need it)
+except ImportError as e:
+    _py_step = _NotBuilt("_py_step", e)
 
 TC_OK = 0
 TC_ERR_INVALID, TC_ERR_UNKNOWN_TABLE, TC_ERR_OOM_POOL = -1, -2, -3
@@ -123,7 +139,8 @@ class TcError(RuntimeError):
         self.code = code
 
 
-_py_step.set_error(TcError)
+if not isinstance(_py_step, _NotBuilt):
+    _py_step.set_error(TcError)
 
 
 def _ptr(x) -> Optional[int]:
