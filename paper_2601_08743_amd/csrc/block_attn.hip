@@ -9,6 +9,7 @@
 
 #include "arrive.h"
 #include "lds_dma.h"
+#include "score_route.h"
 #include "step_ops.h"
 
 namespace tc {
@@ -207,8 +208,6 @@ struct BlockScale {
 // Scores to memory, where one launch for scores and list (below) does not do: a work-group takes a KV head and a range of candidates,
 // a wave 16 blocks at a time.  Ranges come behind one another in the grid: the last ones are short or empty, and as neighbours
 // each would belong to chiplets of its own (the case of many tokens below: 28 us).
-constexpr int kScoreBlocks = 256;                        // candidates of a work-group
-
 // One token (its heads 16 at a time): tokens of many requests, long tables (four tokens, 8 KV heads, 1.4 to 1.7 k blocks: 5.9 us).
 template <bool kBf16, int kD>
 __global__ __launch_bounds__(256) void score_token_kernel(Geom g, SelectArgs a)
@@ -714,10 +713,9 @@ static hipError_t launch_score_select(const Geom &g, const SelectArgs &a, const 
 template <bool kBf16, int kD>
 static hipError_t launch_scores(const Geom &g, SelectArgs a, const Launch &L)
 {
-    // several tokens a work-group where requests bring more than one each
-    const bool grouped = a.n_tokens > a.B && g.G <= 16;
-    a.group_tokens = grouped ? 4 * (16 / g.G) : 1;
-    a.score_parts = (a.max_blocks + kScoreBlocks - 1) / kScoreBlocks;
+    const bool grouped = scores_by_group(a.n_tokens, a.B, g.G, g.Hkv, a.max_blocks);
+    a.group_tokens = grouped ? score_group_tokens(g.G) : 1;
+    a.score_parts = (int32_t)score_parts(a.max_blocks);
     const int64_t grid = (int64_t)((a.n_tokens + a.group_tokens - 1) / a.group_tokens) * g.Hkv * a.score_parts;
     if (grid > kStepMaxGroups) return hipErrorInvalidValue;
     a.parts = FastDiv((uint32_t)(grid / a.score_parts));
@@ -726,7 +724,7 @@ static hipError_t launch_scores(const Geom &g, SelectArgs a, const Launch &L)
     return hipGetLastError();
 }
 
-int64_t select_groups(int Hkv, int max_blocks) { return (int64_t)Hkv * std::max(1, (max_blocks + kScoreBlocks - 1) / kScoreBlocks); }
+int64_t select_groups(int Hkv, int max_blocks) { return (int64_t)Hkv * std::max<int64_t>(1, score_parts(max_blocks)); }
 
 hipError_t launch_select(const Geom &g, SelectArgs a, const Launch &L)
 {

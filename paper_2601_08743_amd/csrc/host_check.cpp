@@ -19,12 +19,15 @@
 //                                      one line "i q kvh m0 tile_begin tile_end split n_splits arrival part0 part_stride item" per item (arrival: its row tile's counter; item: the one that holds it where counters have no place of their own),
 //                                      "ints <size of the device copy> <compact> <where counters begin> <their size>", "parts <floats> <stride>" and, where a launch merges partials by row, the table that it goes by,
 //                                      "folds <0 or 1>", "merges <0 or 1>" (partials by row are combined inside the launch, by a merge launch), "part_f32 <0 or 1>", "groups <entries> <n_groups>" and one line "g kvh m0 n_splits cu S part0" per merge group
+//   scores <tokens> <table rows> <G> <Hkv> <max_blocks>
+//                                   -> "scores <0, or 1: tokens share work-groups> <tokens of one>"
 //   trie <n> then n lines "<id> <len> tok..."; match <len> tok... -> "match <n> (id start)..."
 //   rerank <n_queries> <n_tables> <anchor> then per query "<k> ids..." -> "rerank order..."
 //   pipeline <n_queries> <capacity> <b_c> <b_m> <keep_pinned> <taper> then per query "<k> ids..."
 //                                   -> "pipeline <n_steps | status>" and one line of six numbers per step
 #include "host_logic.h"
 #include "frontend.hip"
+#include "score_route.h"
 
 #include <cstdio>
 #include <iostream>
@@ -154,6 +157,10 @@ int main()
             std::printf("part_f32 %d\n", p.part_f32 ? 1 : 0);
             std::printf("groups %d %d\n", (int)groups.size(), p.n_groups);
             for (const MergeGroup &mg : groups) std::printf("g %d %d %d %d %d %d\n", mg.kvh, mg.m0, mg.n_splits, mg.cu, mg.S, mg.part0);
+        } else if (cmd == "scores") {
+            int64_t n, rows, G, Hkv, mb;
+            std::cin >> n >> rows >> G >> Hkv >> mb;
+            std::printf("scores %d %d\n", scores_by_group(n, rows, (int)G, (int)Hkv, mb) ? 1 : 0, score_group_tokens((int)G));
         } else if (cmd == "trie") {
             int n;
             std::cin >> n;
