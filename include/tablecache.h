@@ -461,6 +461,7 @@ tc_status tc_select_blocks(tc_ctx *ctx, int32_t layer, const void *q, const int3
  *                 layer or an earlier one) or of the caller's own making.  -1, blocks behind the token's own and entries that
  *                 name no block are passed over; a block listed twice is attended to twice.
  *   out           [n_tokens][Hq][D]; rows whose request or position is none are left as they are
+ *   sm_scale      positive, and finite times log2(e)
  * The workspace holds partial results where few tokens' long lists are shared out over work-groups.
  * Errors: TC_ERR_INVALID; TC_ERR_CAPACITY (workspace).
  */

@@ -1338,7 +1338,8 @@ tc_status tc_block_attn(tc_ctx *ctx, int32_t layer, const void *q, const int32_t
     tc_status st = step_check(ctx, "block attn", n_tokens, B, max_blocks);
     if (st == TC_OK) st = layer_check(ctx, "block attn", layer);
     if (st != TC_OK) return st;
-    if (!(sm_scale > 0.f) || !std::isfinite(sm_scale)) return fail(ctx, TC_ERR_INVALID, "block attn: sm_scale must be positive and finite");
+    const float scale_log2 = sm_scale * 1.4426950408889634f;             // (of weights as powers of two)
+    if (!(sm_scale > 0.f) || !std::isfinite(scale_log2)) return fail(ctx, TC_ERR_INVALID, "block attn: sm_scale must be positive, and finite times log2(e)");
     if (n_list < 1 || n_list > (1 << 26)) return fail(ctx, TC_ERR_INVALID, "block attn: lists of %d blocks", n_list);
     if (n_tokens == 0) return TC_OK;
     if (!q || !token_seq || !token_pos || !lists || !out || ((int64_t)B * max_blocks > 0 && !block_table))
@@ -1352,7 +1353,7 @@ tc_status tc_block_attn(tc_ctx *ctx, int32_t layer, const void *q, const int32_t
         return fail(ctx, TC_ERR_CAPACITY, "block attn: the workspace holds %zu bytes, the partials take %zu", workspace ? workspace_bytes : 0, need);
     BlockAttnArgs a{};
     a.q = (const char *)q; a.token_seq = token_seq; a.token_pos = token_pos; a.block_table = block_table; a.lists = lists;
-    a.out = (char *)out; a.scale_log2 = sm_scale * 1.4426950408889634f;
+    a.out = (char *)out; a.scale_log2 = scale_log2;
     a.n_tokens = n_tokens; a.layer = layer; a.B = B; a.max_blocks = max_blocks; a.n_list = n_list;
     a.n_splits = splits;
     a.first_block = (int32_t)first_pool_block(ctx->cfg);
