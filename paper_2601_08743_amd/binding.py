@@ -5,7 +5,8 @@ Every function here has the name of the C entry point it calls (see
 include/tablecache.h for the semantics).  Device tensors are passed as torch
 tensors (their ``data_ptr()`` is used) or raw integer addresses; host integer
 arrays are numpy int32.  There is no fallback: if the library has not been
-built, importing this module raises.
+built, importing this module raises; if only the token steps' module has not,
+those calls do.
 """
 from __future__ import annotations
 

@@ -208,7 +208,8 @@ struct BlockScale {
 // Scores to memory, where one launch for scores and list (below) does not do: a work-group takes a KV head and a range of candidates,
 // a wave 16 blocks at a time.  Ranges come behind one another in the grid: the last ones are short or empty, and as neighbours
 // each would belong to chiplets of its own (the case of many tokens below: 28 us).
-// One token (its heads 16 at a time): tokens of many requests, long tables (four tokens, 8 KV heads, 1.4 to 1.7 k blocks: 5.9 us).
+// One token (its heads 16 at a time): tokens of many requests, long tables (four tokens, 8 KV heads, 1.4 to 1.7 k blocks: 9.5 us with the
+// lists).
 template <bool kBf16, int kD>
 __global__ __launch_bounds__(256) void score_token_kernel(Geom g, SelectArgs a)
 {
@@ -274,7 +275,8 @@ __global__ __launch_bounds__(256) void score_token_kernel(Geom g, SelectArgs a)
 }
 
 // 4 (16 / G) neighbouring tokens, four tiles of query rows: suffixes, whose tokens read the same digests.  Tokens of another request
-// follow with a pass of their own.  (681 tokens of eight requests, 8 KV heads, 380 to 849 blocks: 21.8 us.)  The products of rows 4 q4 + e of tile t stand in quarter q4 of a wave, so these sixteen
+// follow with a pass of their own.  (681 tokens of eight requests, 8 KV heads, 380 to 849 blocks: 31 us with the lists, of which the
+// profiler, under which both launches are slower, gives this one 22 of 36.)  The products of rows 4 q4 + e of tile t stand in quarter q4 of a wave, so these sixteen
 // are the heads of 16 / G whole tokens, one after the other, and a token's largest is found in registers.
 constexpr int kTiles = 4;
 
@@ -466,10 +468,10 @@ __device__ __forceinline__ void pick(PickShared<kThreads, kAll> &s, const uint32
     }
 }
 
-// Lists from scores in memory: a work-group a (token, KV head).
-//   kThreads 256: eight candidates a thread, 1024 bins, a chain of barriers (32 items, 118 of 1.7 k each: 5.6 us)
+// Lists from scores in memory: a work-group a (token, KV head).  Times of this launch under the profiler, of passes without it:
+//   kThreads 256: eight candidates a thread, 1024 bins, a chain of barriers (32 items, 118 of 1.7 k each: 5.9 us)
 //   kThreads 64: a wave, which waits for no other, up to 16 a thread, 256 bins.  Longer from start to end, but beyond four waves a CU
-//   what counts is what they do together (5.4 k items, 60 of some 600: 14.2 us, 17.6 by 256 threads; a pass of scores, list and
+//   what counts is what they do together (5.4 k items, 60 of some 600: 14.3 us, 17.6 by 256 threads; a pass of scores, list and
 //   attention for 640 items 41.0 against 39.6, for 1088 50.0 against 50.5, for 15 k 325 against 341)
 constexpr int kSelectWave = 64 * 16, kSelectFew = 256 * 8;              // table entries that each does for
 constexpr int kSelectItems = 1024;
@@ -612,7 +614,8 @@ __global__ __launch_bounds__(256) void select_long_kernel(Geom g, SelectArgs a)
 // Scores and list in one launch, for few tokens whose tables are not long: a work-group of sixteen waves a (token, KV head), the
 // scores in LDS.  A CU takes its digests at some 80 GB/s, so beyond kFusedBlocks table entries launches that spread them over the chip
 // are as good or better (four tokens of 8 KV heads, 1.7 k entries: 12.4 us so, 12.0 in two), and many tokens of a request should
-// read them once (above kFusedItems).  One token of 4 KV heads, 288 entries: 6.0 us; 32 tokens of up to 311: 7.4.
+// read them once (above kFusedItems).  One token of 4 KV heads, 288 entries: 6.6 us a call;
+// 32 tokens of up to 311: 7.0.
 constexpr int kFusedBlocks = 1536, kFusedItems = 512;
 
 template <bool kBf16, int kD>
@@ -809,8 +812,9 @@ __device__ __forceinline__ int listed_keys(const Geom &g, const BlockAttnArgs &a
 // from there: loaded straight into the operands' registers, where neighbouring lanes are neighbouring rows of 256 bytes, keys take a
 // CU's address path 64 cycles a kilobyte instead of 16.  The next unit's keys are requested as soon as this one's are in
 // registers, and so the values.  (Values straight to registers, 32-byte rows, and twice the waves: slower for every list tried.)
-// Bound: 53 blocks for each of 4 items, 7.2 us, what one CU takes; 49 for each of 128, 51 MB, 10.9 us = 4.7 TB/s, likewise;
-// 64 for each of 5.4 k items, 155 us, the L2's 2.8 GB = 18 TB/s, of which a fifth comes from further (all there: 105 us).
+// Bound: 53 blocks for each of 4 items, 7.7 us a call, what one CU takes; 49 for each of 128, 51 MB, 11.8 us = 4.4 TB/s, likewise;
+// 64 for each of 5.4 k items, 151 us, 2.9 GB through the L2s = 19 TB/s, of which a fifth misses there (counters: 22.6 M requests of 128
+// bytes, 4.7 M misses).
 constexpr int kBaBlock = 4096;                           // one head's K (or V) in one block
 constexpr int kBaWaves = 4;
 constexpr int kBaWave = 4 * kBaBlock;                    // K of a unit: rows of 256 bytes, 16-byte chunk c of row r at c ^ r; V: two blocks verbatim
@@ -1110,7 +1114,7 @@ __global__ __launch_bounds__(256, 2) void block_attn_f32_kernel(Geom g, BlockAtt
 }
 
 // Ranges of a list combined: kD / 4 threads a row, all of a row's first partials requested at once (bound: the launch and one round trip;
-// 128 rows of four ranges 3.6 us).
+// 128 rows of four ranges 3.7 us under the profiler).
 template <bool kBf16, int kD>
 __global__ __launch_bounds__(256) void block_merge_kernel(Geom g, BlockAttnArgs a)
 {
@@ -1148,13 +1152,14 @@ __global__ __launch_bounds__(256) void block_merge_kernel(Geom g, BlockAttnArgs 
 }
 
 // Ranges of a list.  Four waves to a work-group: two of them share a CU where items fill the chip, and their starts and ends overlap
-// (5.4 k bf16 items of 64 blocks: 155 us; with eight waves 205), and for few items eight waves are no faster.
+// (5.4 k bf16 items of 64 blocks, weights in one part yet: 155 us; with eight waves 205), and for few items eight waves are no faster.
 //   bf16: a work-group reads a list at what a CU takes from memory, some 80 GB/s, so ranges of eight units, two a wave, for work-groups of
-//   their own pay for the launch that combines them (4 us with the gap) where lists are long and few: a pass of scores, list and attention
-//   takes, in ranges and in one, for 8 lists of 80 blocks 13.6 and 15.6 us, of 160 14.7 and 21.2; for 32 of 80 15.2 and 16.8, of 128
-//   17.5 and 21.2; for 48 of 80 17.1 and 17.3, of 160 22.4 and 24.4; for 64 of 160 25.7 and 24.9; for 8 of 44 13.5 and 13.4.
+//   their own pay for the launch that combines them (4 us with the gap) where lists are long and few: a call takes, in ranges and in
+//   one, for 4 lists of 44 blocks 7.4 and 6.9 us, of 56 7.4 and 7.5, of 80 7.6 and 9.1, of 160 8.7 and 14.7; for 32 of 56 8.0 and 7.9, of 80
+//   8.2 and 9.6, of 128 9.5 and 13.2; for 48 of 64 8.7 and 8.7, of 80 9.4 and 10.3, of 160 16.0 and 17.6; for 64 of 80 12.4 and 10.9, of 160
+//   19.6 and 17.8.
 //   fp32: bound by its own vector work, 400 instructions a block of four rows, so a unit a wave up to two work-groups a CU (24 blocks
-//   for each of 20 items 5.3 + 2.8 us; in one range of eight waves 9.8).
+//   for each of 20 items 7.7 us a call; in one range of eight waves 9.8).
 constexpr int kBaRangeItems = 48, kBaRangeUnits = 28;
 
 // 16 rows of a token and KV head, or 8, to a work-group

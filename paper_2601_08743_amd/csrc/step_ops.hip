@@ -14,8 +14,8 @@ namespace tc {
 //
 // Two prefix sums over the requests, of new tokens and of blocks; then a thread for every token, which finds its request by bisection
 // in LDS, four tokens side by side.  Everything is a few kilobytes: a few tokens are a chain of dependent steps, one work-group and
-// one launch (four requests: 3.1 us); of many the instructions count, 150 a token, so each of several work-groups repeats the sums
-// and writes its part (300 requests, 5.0 k tokens: 6.2 us so, 10 in one work-group).  Where the results are to stand in place of
+// one launch (four requests: 3.6 to 4.3 us a call); of many the instructions count, 150 a token, so each of several work-groups repeats the sums
+// and writes its part (300 requests, 5.0 k tokens: 5.9 us so, 10 in one work-group).  Where the results are to stand in place of
 // the inputs that the other work-groups still read, the sums are a launch of their own and the second takes the lengths from its
 // results.
 //
@@ -205,8 +205,8 @@ hipError_t launch_step_tables(const StepTables &s, const Launch &L)
 // A work-group a token: its (cos, sin) table in LDS, then a thread for every pair of 16-byte chunks.  The values of a bf16 block are
 // stored transposed, two bytes of a token in each row of 32; tokens that go to the same block therefore share its KV heads
 // out among their work-groups, each of which takes those heads' rows of all of them and writes whole rows.  Bound: memory, for many tokens
-// (2048, 32 / 8 heads, 50 MB: 10.8 us = 4.7 TB/s; 21.8 with two-byte stores); slot, position and row one after the other for few
-// (32 tokens 4.5 us).
+// (2048, 32 / 8 heads, 50 MB: 11.0 us = 4.6 TB/s; 21.8 with two-byte stores); for few the chain that a work-group makes of
+// slot, position and row, though all three follow from the token's number (32 tokens 4.6 us).
 struct Run { int first, len; };                          // the step's tokens of one block
 
 // The tokens around token n (slot `slot`) that stand behind one another in the same block: one load for the wave.
