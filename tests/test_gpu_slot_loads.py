@@ -19,9 +19,9 @@ class Busy:
         torch.mm(self.a, self.a, out=self.b)
         torch.cuda.synchronize()
 
-    def on(self, stream):
+    def on(self, stream, times=12):
         with torch.cuda.stream(stream):
-            for _ in range(12):
+            for _ in range(times):
                 torch.mm(self.a, self.a, out=self.b)
 
 
@@ -148,8 +148,9 @@ def test_steps_on_many_streams_do_not_make_a_load_wait_on_the_host():
     streams = [torch.cuda.default_stream()] + [torch.cuda.Stream() for _ in range(32)]
     assert len({s.cuda_stream for s in streams}) == 33
     steps = [_step_arrays(dw, wl, bt, pl) for _ in streams]
+    _attend(dw, steps[0], streams[0])           # (what a first call sets up)
     torch.cuda.synchronize()
-    busy.on(streams[7])
+    busy.on(streams[7], 40)
     done = []
     for st, s in zip(streams, steps):
         _attend(dw, s, st)
